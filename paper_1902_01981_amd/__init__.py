@@ -1,2 +1,12 @@
-"""MI355X-native CodedReduce hot path: thin ctypes binding over libcodedreduce.so (argument marshalling only)."""
+"""MI355X-native CodedReduce hot path and network layers: thin ctypes bindings over libcodedreduce.so and libcodedreduce_layers.so (argument
+marshalling only).  The layers' binding, which needs torch, is imported when one of its names is first asked for."""
 from .api import *  # noqa: F401,F403
+
+
+def __getattr__(name):
+    if name.startswith(("cr_", "CR_ACT_", "LAYERS_", "load_layers")):
+        from . import layers
+
+        if hasattr(layers, name):
+            return getattr(layers, name)
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

@@ -1,4 +1,4 @@
-"""Builds libcodedreduce.so (host plan + C-ABI + gfx950 kernels) in-tree with hipcc."""
+"""Builds libcodedreduce.so (host plan + C-ABI + gfx950 kernels) and libcodedreduce_layers.so (layers of networks) in-tree with hipcc."""
 from __future__ import annotations
 
 import os
@@ -10,16 +10,23 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcodedreduce.so")
 SOURCES = ["gc_design.cpp", "tree_plan.cpp", "latency_model.cpp", "codedreduce.cpp", "kernels.hip"]
+LAYERS_LIB = os.path.join(HERE, "libcodedreduce_layers.so")
+LAYERS_SOURCES = ["layers.cpp", "norm_kernels.hip", "dropout_kernels.hip", "loss_kernels.hip"]
 # the packed-fp32 target feature is switched off for all device code
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
 def build(verbose: bool = False) -> str:
+    _library(LAYERS_LIB, LAYERS_SOURCES, verbose)
+    return _library(LIB, SOURCES, verbose)
+
+
+def _library(lib: str, sources, verbose: bool) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     bdir = os.path.join(HERE, "_build")
     os.makedirs(bdir, exist_ok=True)
     objs = []
-    for src in SOURCES:
+    for src in sources:
         obj = os.path.join(bdir, src + ".o")
         cmd = [hipcc, "-O3", "-std=c++17", "-fPIC", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
         if src.endswith(".hip"):
@@ -30,8 +37,8 @@ def build(verbose: bool = False) -> str:
         _run(cmd, verbose)
         objs.append(obj)
     # the interface and nothing else: helpers with plain names would meet a program's own
-    _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-Wl,--version-script=" + os.path.join(CSRC, "exports.map"), "-o", LIB] + objs, verbose)
-    return LIB
+    _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-Wl,--version-script=" + os.path.join(CSRC, "exports.map"), "-o", lib] + objs, verbose)
+    return lib
 
 
 def _run(cmd, verbose):

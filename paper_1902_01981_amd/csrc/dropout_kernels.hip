@@ -1,117 +1,312 @@
 // Bias, dropout and residual, the mask drawn from a counter, for gfx950.
-#include "layers_device.h"
-
-#include <algorithm>
+//
+// A word of 64 bits has the draws of four neighbouring channels.  Word number i is mix(key + (i + 1) golden): from row to row a thread's number
+// moves on by a constant, so that golden times it is one 64-bit addition, and a word costs the two products of the mixing function.
+//
+//   dropout_forward_kernel, dropout_backward_kernel   a thread has a chunk of 16 bytes of channels and goes down the rows, four at a time; bias and sums
+//                          of the bias's gradient stay in its registers
+//   sum_pieces_kernel      the bias's gradient per run
+#include "runs_device.h"
 
 namespace cr {
 
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kRowsAtOnce = 4;
 
 __device__ __forceinline__ uint64_t mask_key(const Mask &m) { return splitmix_mix(m.key_state + (m.draw_dev ? kGolden * *m.draw_dev : 0)); }
-// the word with the draws of channels [4 word, 4 word + 4) of a row
-__device__ __forceinline__ uint64_t mask_word(const Mask &m, uint64_t key, int64_t n, int positions, int p, int words, int word)
+__device__ __forceinline__ bool kept(uint64_t word, int field, uint32_t least)
 {
-    const uint64_t point = m.point_dev ? m.point_dev[n] : m.first_point + n;
-    return splitmix_mix(key + ((point * positions + p) * words + word + 1) * kGolden);
+    const uint32_t half = field < 2 ? static_cast<uint32_t>(word) : static_cast<uint32_t>(word >> 32);
+    return field % 2 ? half >= least << 16 : (half & 0xffffu) >= least;      // the low half decides nothing: least << 16 ends in zeros
 }
-__device__ __forceinline__ bool kept(uint64_t word, int field, uint32_t least) { return (static_cast<uint32_t>(word >> (16 * field)) & 0xffffu) >= least; }
 
-// a thread per word of the mask
-template <bool BF16> __global__ void __launch_bounds__(kThreads) dropout_forward_kernel(DropoutArgs a)
+// The columns that a workgroup has: `across` chunks from first_chunk on, rows side by side in the rest of its threads; the last of a row of workgroups also
+// has the `left` channels behind the whole chunks, an element per thread.
+struct Columns {
+    int chunks, across, down;    // whole chunks of a row, chunks of a workgroup, rows side by side
+};
+Columns columns_of(int channels, int vec)
 {
+    Columns c;
+    c.chunks = channels / vec;
+    const int tiles = std::max(1, (c.chunks + kThreads - 1) / kThreads);
+    c.across = (c.chunks + tiles - 1) / tiles;
+    c.down = c.across ? kThreads / c.across : kThreads;
+    return c;
+}
+int tiles_of(const Columns &c) { return c.across ? (c.chunks + c.across - 1) / c.across : 1; }
+
+// Where row r of all points' positions lies, and the number of its first word.  FLAT: rows have one stride and the points follow each other.
+template <bool FLAT> struct RowWalk {
+    const Mask &mask;
+    int positions;
+    __device__ __forceinline__ int64_t at(const Rows &v, int64_t r) const
+    {
+        if (FLAT) return r * v.position_stride;
+        return r / positions * v.point_stride + r % positions * v.position_stride;
+    }
+    __device__ __forceinline__ uint64_t number(int64_t r) const          // of the row among all rows of all data points
+    {
+        if (FLAT || !mask.point_dev) return static_cast<uint64_t>(mask.first_point) * positions + r;
+        return static_cast<uint64_t>(mask.point_dev[r / positions]) * positions + r % positions;
+    }
+};
+
+template <bool BF16, bool FLAT, bool RESIDUAL>
+__global__ void __launch_bounds__(kThreads) dropout_forward_kernel(DropoutArgs a, Columns c, int64_t length)
+{
+    constexpr int VEC = BF16 ? 8 : 4, U = kRowsAtOnce;
+    using C = Chunk<BF16, VEC>;
     using E = Element<BF16>;
-    using T = typename E::type;
+    using T = typename C::element;
+    const RowWalk<FLAT> walk = {a.mask, a.shape.positions};
     const int words = (a.shape.channels + 3) / 4;
+    const int64_t begin = blockIdx.y * length, end = min(begin + length, a.shape.points * a.shape.positions);
     const uint64_t key = mask_key(a.mask);
-    const int64_t total = a.shape.points * a.shape.positions * words;
-    for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kThreads) {
-        const int word = static_cast<int>(i % words), p = static_cast<int>(i / words % a.shape.positions);
-        const int64_t n = i / words / a.shape.positions;
-        const uint64_t z = mask_word(a.mask, key, n, a.shape.positions, p, words, word);
-        for (int f = 0; f < 4 && 4 * word + f < a.shape.channels; ++f) {
-            const int c = 4 * word + f;
-            float v = 0.f;
-            if (kept(z, f, a.mask.least))
-                v = (E::get(static_cast<const T *>(a.x.p) + n * a.x.point_stride + p * a.x.position_stride + c) + (a.bias ? a.bias[c] : 0.f)) * a.mask.scale;
-            if (a.residual.p) v += E::get(static_cast<const T *>(a.residual.p) + n * a.residual.point_stride + p * a.residual.position_stride + c);
-            E::put(static_cast<T *>(a.y.p) + n * a.y.point_stride + p * a.y.position_stride + c, v);
+    const T *x = static_cast<const T *>(a.x.p), *residual = static_cast<const T *>(a.residual.p);
+    T *y = static_cast<T *>(a.y.p);
+
+    const int across = min(c.across, c.chunks - static_cast<int>(blockIdx.x) * c.across);
+    const int tx = threadIdx.x % max(c.across, 1), ty = threadIdx.x / max(c.across, 1);
+    if (tx < across && ty < c.down) {
+        const int channel = (blockIdx.x * c.across + tx) * VEC;
+        float bias[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) bias[v] = a.bias ? a.bias[channel + v] : 0.f;
+        for (int64_t r0 = begin + ty; r0 < end; r0 += U * c.down) {
+            typename C::raw in[U], add[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = min(r0 + u * c.down, end - 1);
+                in[u] = C::load_once(x + walk.at(a.x, r) + channel);
+                if constexpr (RESIDUAL) add[u] = C::load_once(residual + walk.at(a.residual, r) + channel);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = r0 + u * c.down;
+                if (r >= end) break;
+                float v[VEC], s[VEC];
+                C::widen(in[u], v);
+                if constexpr (RESIDUAL) C::widen(add[u], s);
+                const uint64_t state = key + (walk.number(r) * words + channel / 4 + 1) * kGolden;
+#pragma unroll
+                for (int w = 0; w < VEC / 4; ++w) {
+                    const uint64_t word = splitmix_mix(state + w * kGolden);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const int i = 4 * w + f;
+                        const float t = kept(word, f, a.mask.least) ? (v[i] + bias[i]) * a.mask.scale : 0.f;
+                        v[i] = RESIDUAL ? s[i] + t : t;
+                    }
+                }
+                C::store(y + walk.at(a.y, r) + channel, C::narrow(v));
+            }
+        }
+    }
+    const int left = a.shape.channels - c.chunks * VEC;
+    if (left > 0 && blockIdx.x == gridDim.x - 1) {
+        for (int64_t i = threadIdx.x; i < (end - begin) * left; i += kThreads) {
+            const int64_t r = begin + i / left;
+            const int channel = c.chunks * VEC + static_cast<int>(i % left);
+            const uint64_t word = splitmix_mix(key + (walk.number(r) * words + channel / 4 + 1) * kGolden);
+            float t = kept(word, channel % 4, a.mask.least) ? (E::get(x + walk.at(a.x, r) + channel) + (a.bias ? a.bias[channel] : 0.f)) * a.mask.scale : 0.f;
+            if constexpr (RESIDUAL) t += E::get(residual + walk.at(a.residual, r) + channel);
+            E::put(y + walk.at(a.y, r) + channel, t);
         }
     }
 }
 
-template <bool BF16> __global__ void __launch_bounds__(kThreads) dropout_dx_kernel(DropoutGradArgs a)
+// dx, and the sums of a piece's columns into its row of parts.
+template <bool BF16, bool FLAT, bool DX, bool SUMS>
+__global__ void __launch_bounds__(kThreads) dropout_backward_kernel(DropoutGradArgs a, Columns c, Pieces pieces, float *parts)
 {
+    constexpr int VEC = BF16 ? 8 : 4, U = kRowsAtOnce;
+    using C = Chunk<BF16, VEC>;
     using E = Element<BF16>;
-    using T = typename E::type;
+    using T = typename C::element;
+    __shared__ float lds[kThreads * VEC];
+    const RowWalk<FLAT> walk = {a.mask, a.shape.positions};
     const int words = (a.shape.channels + 3) / 4;
+    const Piece piece = find_piece(pieces, blockIdx.y);
     const uint64_t key = mask_key(a.mask);
-    const int64_t total = a.shape.points * a.shape.positions * words;
-    for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kThreads) {
-        const int word = static_cast<int>(i % words), p = static_cast<int>(i / words % a.shape.positions);
-        const int64_t n = i / words / a.shape.positions;
-        const uint64_t z = mask_word(a.mask, key, n, a.shape.positions, p, words, word);
-        for (int f = 0; f < 4 && 4 * word + f < a.shape.channels; ++f) {
-            const int c = 4 * word + f;
-            const float v = kept(z, f, a.mask.least) ? E::get(static_cast<const T *>(a.dy.p) + n * a.dy.point_stride + p * a.dy.position_stride + c) * a.mask.scale : 0.f;
-            E::put(static_cast<T *>(a.dx.p) + n * a.dx.point_stride + p * a.dx.position_stride + c, v);
+    const T *dy = static_cast<const T *>(a.dy.p);
+    T *dx = static_cast<T *>(a.dx.p);
+
+    const int across = min(c.across, c.chunks - static_cast<int>(blockIdx.x) * c.across);
+    const int tx = threadIdx.x % max(c.across, 1), ty = threadIdx.x / max(c.across, 1);
+    const int channel = (blockIdx.x * c.across + tx) * VEC;
+    float sum[VEC];
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sum[v] = 0.f;
+    if (tx < across && ty < c.down) {
+        for (int64_t r0 = piece.begin + ty; r0 < piece.end; r0 += U * c.down) {
+            typename C::raw in[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) in[u] = C::load_once(dy + walk.at(a.dy, min(r0 + u * c.down, piece.end - 1)) + channel);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t r = r0 + u * c.down;
+                if (r >= piece.end) break;
+                float v[VEC];
+                C::widen(in[u], v);
+                const uint64_t state = key + (walk.number(r) * words + channel / 4 + 1) * kGolden;
+#pragma unroll
+                for (int w = 0; w < VEC / 4; ++w) {
+                    const uint64_t word = splitmix_mix(state + w * kGolden);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f) {
+                        const int i = 4 * w + f;
+                        v[i] = kept(word, f, a.mask.least) ? v[i] * a.mask.scale : 0.f;
+                        sum[i] += v[i];
+                    }
+                }
+                if constexpr (DX) C::store(dx + walk.at(a.dx, r) + channel, C::narrow(v));
+            }
+        }
+    }
+    if constexpr (SUMS) {
+        if (c.across > 0) {
+            const int width = c.across * VEC;
+            if (ty < c.down) {
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) lds[ty * width + tx * VEC + v] = sum[v];
+            }
+            // columns' sums, side by side by as many threads as there are, then by one each
+            const int shares = max(1, kThreads / width);
+            __syncthreads();
+            float s = 0.f;
+            if (shares > 1) {
+                const int col = threadIdx.x % width, share = threadIdx.x / width;
+                if (share < shares)
+                    for (int r = share; r < c.down; r += shares) s += lds[r * width + col];
+                __syncthreads();
+                if (share < shares) lds[share * width + col] = s;
+                __syncthreads();
+            }
+            const int rows = shares > 1 ? min(shares, c.down) : c.down;
+            for (int col = threadIdx.x; col < across * VEC; col += kThreads) {
+                s = 0.f;
+                for (int r = 0; r < rows; ++r) s += lds[r * width + col];
+                parts[int64_t(blockIdx.y) * a.shape.channels + blockIdx.x * width + col] = s;
+            }
+        }
+    }
+    const int left = a.shape.channels - c.chunks * VEC;
+    if (left > 0 && blockIdx.x == gridDim.x - 1) {
+        // a thread stays with its channel: rows side by side in what a multiple of `left` threads leaves
+        const int down = kThreads / left, i = threadIdx.x % left;
+        const int at = c.chunks * VEC + i;
+        float s = 0.f;
+        if (static_cast<int>(threadIdx.x) < down * left) {
+            for (int64_t r = piece.begin + threadIdx.x / left; r < piece.end; r += down) {
+                const uint64_t word = splitmix_mix(key + (walk.number(r) * words + at / 4 + 1) * kGolden);
+                const float t = kept(word, at % 4, a.mask.least) ? E::get(dy + walk.at(a.dy, r) + at) * a.mask.scale : 0.f;
+                s += t;
+                if constexpr (DX) E::put(dx + walk.at(a.dx, r) + at, t);
+            }
+        }
+        if constexpr (SUMS) {
+            __syncthreads();
+            lds[threadIdx.x] = s;
+            __syncthreads();
+            if (static_cast<int>(threadIdx.x) < left) {
+                s = 0.f;
+                for (int d = 0; d < down; ++d) s += lds[d * left + threadIdx.x];
+                parts[int64_t(blockIdx.y) * a.shape.channels + at] = s;
+            }
         }
     }
 }
 
-// a workgroup per channel and run; before dx, which may replace dy
-template <bool BF16> __global__ void __launch_bounds__(kThreads) dropout_bias_kernel(DropoutGradArgs a, RunTable table, int64_t first_run)
+constexpr int kUnits = 256;
+
+// rows of a workgroup: enough workgroups to fill the chip several times, and a few steps for each
+int64_t rows_of_workgroup(int64_t rows, const Columns &c, int workgroups_per_unit, int steps)
 {
-    using E = Element<BF16>;
-    using T = typename E::type;
-    __shared__ float lds[kThreads / 64];
-    const int r = blockIdx.y, words = (a.shape.channels + 3) / 4;
-    for (int c = blockIdx.x; c < a.shape.channels; c += gridDim.x) {
-    const uint64_t key = mask_key(a.mask);
-    const int64_t begin = int64_t(table.first[r]) * a.shape.positions, end = int64_t(table.first[r + 1]) * a.shape.positions;
-    float sum = 0.f;
-    for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
-        const int64_t n = i / a.shape.positions;
-        const int p = static_cast<int>(i % a.shape.positions);
-        if (kept(mask_word(a.mask, key, n, a.shape.positions, p, words, c / 4), c % 4, a.mask.least))
-            sum += E::get(static_cast<const T *>(a.dy.p) + n * a.dy.point_stride + p * a.dy.position_stride + c) * a.mask.scale;
-    }
-    sum = block_total<kThreads>(sum, lds);
-    if (threadIdx.x == 0) a.dbias[(first_run + r) * a.shape.channels + c] = sum;
-    }
+    const int64_t step = int64_t(c.down) * kRowsAtOnce;
+    const int64_t wanted = std::max<int64_t>(1, kUnits * workgroups_per_unit / tiles_of(c));
+    int64_t length = (rows + wanted - 1) / wanted;
+    length = (length + step - 1) / step * step;
+    length = std::max<int64_t>(length, std::min(step * steps, (rows + step - 1) / step * step));
+    return std::max<int64_t>(length, 1);
 }
 
-unsigned grid_for(const LayerShape &s)
+bool one_stride(const Rows &v, const LayerShape &s) { return s.points <= 1 || s.positions == 1 || v.point_stride == v.position_stride * s.positions; }
+// with one position per point it is the points that have the stride
+Rows flattened(Rows v, const LayerShape &s)
 {
-    const int64_t words = s.points * s.positions * ((s.channels + 3) / 4);
-    return static_cast<unsigned>(std::min<int64_t>((words + kThreads - 1) / kThreads, 256 * 32));
+    if (s.positions == 1) v.position_stride = v.point_stride;
+    return v;
+}
+
+int64_t piece_length(const LayerShape &shape)
+{
+    const Columns c = columns_of(shape.channels, shape.bf16 ? 8 : 4);
+    return rows_of_workgroup(shape.points * shape.positions, c, 4, 4);
 }
 
 }  // namespace
 
-size_t dropout_backward_bytes(const LayerShape &, const int64_t *, int) { return 0; }
-
-hipError_t launch_dropout_forward(const DropoutArgs &a, hipStream_t stream)
+size_t dropout_backward_bytes(const LayerShape &shape, const int64_t *bounds, int runs)
 {
-    if (a.shape.points == 0) return hipSuccess;
-    (a.shape.bf16 ? dropout_forward_kernel<true> : dropout_forward_kernel<false>)<<<grid_for(a.shape), kThreads, 0, stream>>>(a);
+    return static_cast<size_t>(most_pieces(bounds, runs, shape.positions, piece_length(shape))) * shape.channels * sizeof(float);
+}
+
+hipError_t launch_dropout_forward(const DropoutArgs &args, hipStream_t stream)
+{
+    if (args.shape.points == 0) return hipSuccess;
+    DropoutArgs a = args;
+    const bool residual = a.residual.p != nullptr;
+    const bool flat = !a.mask.point_dev && one_stride(a.x, a.shape) && one_stride(a.y, a.shape) && (!residual || one_stride(a.residual, a.shape));
+    if (flat) {
+        a.x = flattened(a.x, a.shape);
+        a.y = flattened(a.y, a.shape);
+        a.residual = flattened(a.residual, a.shape);
+    }
+    const Columns c = columns_of(a.shape.channels, a.shape.bf16 ? 8 : 4);
+    const int64_t rows = a.shape.points * a.shape.positions, length = rows_of_workgroup(rows, c, 16, 1);
+    const dim3 grid(tiles_of(c), static_cast<unsigned>((rows + length - 1) / length));
+    auto pick = [&](auto bf16, auto is_flat) {
+        constexpr bool B = decltype(bf16)::value, F = decltype(is_flat)::value;
+        (residual ? dropout_forward_kernel<B, F, true> : dropout_forward_kernel<B, F, false>)<<<grid, kThreads, 0, stream>>>(a, c, length);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    a.shape.bf16 ? flat ? pick(Yes(), Yes()) : pick(Yes(), No()) : flat ? pick(No(), Yes()) : pick(No(), No());
     return hipGetLastError();
 }
 
-hipError_t launch_dropout_backward(const DropoutGradArgs &a, void *, hipStream_t stream)
+hipError_t launch_dropout_backward(const DropoutGradArgs &args, void *workspace, hipStream_t stream)
 {
-    if (a.dbias) {
-        for (int r = 0; r < a.runs; r += RunTable::kRuns) {
-            RunTable table;
-            table.runs = std::min(RunTable::kRuns, a.runs - r);
-            for (int i = 0; i <= table.runs; ++i) table.first[i] = static_cast<int>(a.bounds[r + i]);
-            const dim3 grid(std::min(a.shape.channels, 1 << 15), table.runs);
-            (a.shape.bf16 ? dropout_bias_kernel<true> : dropout_bias_kernel<false>)<<<grid, kThreads, 0, stream>>>(a, table, r);
-        }
+    DropoutGradArgs a = args;
+    if (!a.dx.p && !a.dbias) return hipSuccess;
+    const bool flat = !a.mask.point_dev && one_stride(a.dy, a.shape) && (!a.dx.p || one_stride(a.dx, a.shape));
+    if (flat) {
+        a.dy = flattened(a.dy, a.shape);
+        a.dx = flattened(a.dx, a.shape);
     }
-    if (a.dx.p && a.shape.points > 0)
-        (a.shape.bf16 ? dropout_dx_kernel<true> : dropout_dx_kernel<false>)<<<grid_for(a.shape), kThreads, 0, stream>>>(a);
+    const Columns c = columns_of(a.shape.channels, a.shape.bf16 ? 8 : 4);
+    const int64_t length = piece_length(a.shape);
+    float *parts = static_cast<float *>(workspace);
+    for (int r = 0; r < a.runs; r += Pieces::kRuns) {
+        Pieces p;
+        const int count = lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), a.shape.positions, length, &p);
+        if (count > 0) {
+            // far fewer than the grid's second dimension takes: at most one for each wanted workgroup and run
+            const dim3 grid(tiles_of(c), count);
+            auto pick = [&](auto bf16, auto is_flat) {
+                constexpr bool B = decltype(bf16)::value, F = decltype(is_flat)::value;
+                (!a.dbias ? dropout_backward_kernel<B, F, true, false> : a.dx.p ? dropout_backward_kernel<B, F, true, true> : dropout_backward_kernel<B, F, false, true>)
+                    <<<grid, kThreads, 0, stream>>>(a, c, p, parts);
+            };
+            using Yes = std::true_type;
+            using No = std::false_type;
+            a.shape.bf16 ? flat ? pick(Yes(), Yes()) : pick(Yes(), No()) : flat ? pick(No(), Yes()) : pick(No(), No());
+        }
+        if (a.dbias) launch_sum_pieces<false>(parts, nullptr, a.shape.channels, p, a.dbias + int64_t(r) * a.shape.channels, nullptr, stream);
+    }
     return hipGetLastError();
 }
 

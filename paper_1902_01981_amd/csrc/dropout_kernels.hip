@@ -251,7 +251,8 @@ int64_t piece_length(const LayerShape &shape)
 
 size_t dropout_backward_bytes(const LayerShape &shape, const int64_t *bounds, int runs)
 {
-    return static_cast<size_t>(most_pieces(bounds, runs, shape.positions, piece_length(shape))) * shape.channels * sizeof(float);
+    const int64_t pieces = most_pieces(bounds, runs, shape.positions, piece_length(shape));
+    return static_cast<size_t>(pieces + rows_beside(pieces, runs)) * shape.channels * sizeof(float);
 }
 
 hipError_t launch_dropout_forward(const DropoutArgs &args, hipStream_t stream)
@@ -289,7 +290,7 @@ hipError_t launch_dropout_backward(const DropoutGradArgs &args, void *workspace,
     }
     const Columns c = columns_of(a.shape.channels, a.shape.bf16 ? 8 : 4);
     const int64_t length = piece_length(a.shape);
-    float *parts = static_cast<float *>(workspace);
+    float *parts = static_cast<float *>(workspace), *beside = a.dbias ? parts + most_pieces(a.bounds, a.runs, a.shape.positions, length) * a.shape.channels : nullptr;
     for (int r = 0; r < a.runs; r += Pieces::kRuns) {
         Pieces p;
         const int count = lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), a.shape.positions, length, &p);
@@ -305,7 +306,7 @@ hipError_t launch_dropout_backward(const DropoutGradArgs &args, void *workspace,
             using No = std::false_type;
             a.shape.bf16 ? flat ? pick(Yes(), Yes()) : pick(Yes(), No()) : flat ? pick(No(), Yes()) : pick(No(), No());
         }
-        if (a.dbias) launch_sum_pieces<false>(parts, nullptr, a.shape.channels, p, a.dbias + int64_t(r) * a.shape.channels, nullptr, stream);
+        if (a.dbias) launch_sum_pieces(parts, nullptr, a.shape.channels, p, beside, a.dbias + int64_t(r) * a.shape.channels, nullptr, stream);
     }
     return hipGetLastError();
 }

@@ -92,20 +92,39 @@ template <bool BF16> struct Element {
 
 // v of the lane that the cross-lane pattern CTRL pairs this one with inside its row of 16 lanes
 template <int CTRL> __device__ __forceinline__ float dpp(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, false)); }
+// v of the lane 16 or 32 lanes away: rows of 16 lanes exchanged between two copies of v
+template <typename F> __device__ __forceinline__ float fold_16(float v, F f)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+template <typename F> __device__ __forceinline__ float fold_32(float v, F f)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
 // Folds f over each LANES neighbouring lanes (a power of two), for every lane: quad swaps, the mirrored half-row and row (as good as an exchange once
-// the lanes of a half agree), then exchanges between rows; over a whole wavefront the four rows' results are read into scalars.
+// the lanes of a half agree), then exchanges between rows.
 template <int LANES, typename F> __device__ __forceinline__ float fold_lanes(float v, F f)
 {
     if constexpr (LANES >= 2) v = f(v, dpp<0xB1>(v));    // quad_perm [1,0,3,2]
     if constexpr (LANES >= 4) v = f(v, dpp<0x4E>(v));    // quad_perm [2,3,0,1]
     if constexpr (LANES >= 8) v = f(v, dpp<0x141>(v));   // row_half_mirror
     if constexpr (LANES >= 16) v = f(v, dpp<0x140>(v));  // row_mirror
-    if constexpr (LANES == 32) v = f(v, __shfl_xor(v, 16, 64));
-    if constexpr (LANES == 64) {
-        auto of = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
-        v = f(f(of(0), of(16)), f(of(32), of(48)));
-    }
+    if constexpr (LANES >= 32) v = fold_16(v, f);
+    if constexpr (LANES == 64) v = fold_32(v, f);
     return v;
+}
+// The sum over the lanes of a wavefront that are a multiple of `across` apart (a power of two up to 32), for every lane.
+__device__ __forceinline__ float total_every(float v, int across)
+{
+    auto add = [](float a, float b) { return a + b; };
+    if (across <= 8) v += dpp<0x128>(v);                 // row_ror:8
+    if (across <= 4) v += dpp<0x124>(v);                 // row_ror:4
+    if (across <= 2) v += dpp<0x122>(v);                 // row_ror:2
+    if (across <= 1) v += dpp<0x121>(v);                 // row_ror:1
+    if (across <= 16) v = fold_16(v, add);
+    return fold_32(v, add);
 }
 template <int LANES> __device__ __forceinline__ float lanes_total(float v)
 {

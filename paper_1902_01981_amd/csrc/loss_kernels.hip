@@ -214,9 +214,9 @@ template <bool BF16, int K, bool WAVE, bool GRAD> __global__ void __launch_bound
                 s.S = meet[1][threadIdx.x % 16];
             }
             join_lanes<16>(s);
-            s.c = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(s.c)));
-            s.S = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(s.S)));
         }
+        s.c = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(s.c)));       // scalars: branches on them are not divergent
+        s.S = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(s.S)));
     };
     // the gradient of a row, each chunk making place for one of the row at x
     auto form = [&](int64_t of, const RowTarget &now, auto more, const T *x) {

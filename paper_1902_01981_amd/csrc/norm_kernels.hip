@@ -203,6 +203,7 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
 struct Tiling {
     int tiles, slices, unit, across, down, side, threads, k;             // slices begin at multiples of `unit` channels of the group
     int pieces;                  // of a point's positions, down * k each
+    int fold;                    // the seats of a column in a wavefront are `across` lanes apart, and the wavefront has one point's: they are added up before LDS
 };
 struct Columns {
     int group, groups, first, width;                     // of a tile
@@ -245,40 +246,42 @@ template <int VEC> __device__ __forceinline__ Seat take_seat(const Tiling &t, co
     return s;
 }
 
-// Sums over the groups of a tile.  Each thread brings one value, of a chunk that lies in one group (WIDE), or VEC of them, one for each channel; the sum over
-// the rows and the channels of a group goes to out[side * groups + group], where every thread finds it after the call.
-template <int VEC, bool WIDE> struct GroupSum {
-    float *lds;                  // threads * (WIDE ? 1 : VEC) floats
+// Sums over the groups of a tile.  A thread brings a value for each UNIT of its channels, which lie in one group; the sum over the rows and the channels of
+// a group goes to out[side * groups + group], where every thread finds it after the call.
+template <int VEC, int UNIT> struct GroupSum {
+    static constexpr int NV = VEC / UNIT;
+    float *lds;                  // threads * NV floats
     const Tiling &t;
     const Columns &c;
     int cg;
-    __device__ __forceinline__ void put(const Seat &s, const float (&value)[VEC], float *to)
+    __device__ __forceinline__ void put(const Seat &s, const float (&value)[NV], float *to)
     {
-        const int row = s.side * t.down + s.ty;
-        if (!s.has) return;
-        if constexpr (WIDE) {
-            float sum = 0.f;
+        const int width = c.width / UNIT;
+        if (t.fold) {
+            float v[NV];
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) sum += value[v];
-            to[row * (c.width / VEC) + s.at / VEC] = sum;
-        } else {
+            for (int i = 0; i < NV; ++i) v[i] = total_every(value[i], t.across);
+            if (s.has && static_cast<int>(threadIdx.x % 64) < t.across) {
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) to[row * c.width + s.at + v] = value[v];
+                for (int i = 0; i < NV; ++i) to[threadIdx.x / 64 * width + s.at / UNIT + i] = v[i];
+            }
+        } else if (s.has) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) to[(s.side * t.down + s.ty) * width + s.at / UNIT + i] = value[i];
         }
     }
-    // lanes per sum: a power of two, so that the sums share out the workgroup's threads
     __device__ __forceinline__ void add(const float *from, float *out)
     {
-        const int per = WIDE ? cg / VEC : cg, width = WIDE ? c.width / VEC : c.width, sums = t.side * c.groups;
-        int lanes = 64;
+        const int per = cg / UNIT, width = c.width / UNIT, sums = t.side * c.groups, rows = t.fold ? t.down * t.across / 64 : t.down;
+        int lanes = 64;          // per sum: a power of two, so that the sums share out the workgroup's threads
         while (lanes > 1 && lanes * sums > static_cast<int>(blockDim.x)) lanes /= 2;
         const int lane = threadIdx.x % lanes, step_row = lanes / per, step_col = lanes % per;
         for (int q = threadIdx.x / lanes; q < sums; q += blockDim.x / lanes) {
             const int side = q / c.groups, g = q % c.groups;
-            const float *base = from + side * t.down * width + g * per;
+            const float *base = from + side * rows * width + g * per;
             int row = lane / per, col = lane % per;
             float sum = 0.f;
-            while (row < t.down) {
+            while (row < rows) {
                 sum += base[row * width + col];
                 row += step_row;
                 col += step_col;
@@ -291,7 +294,7 @@ template <int VEC, bool WIDE> struct GroupSum {
             if (lane == 0) out[q] = sum;
         }
     }
-    __device__ __forceinline__ void operator()(const Seat &s, const float (&value)[VEC], float *out)
+    __device__ __forceinline__ void operator()(const Seat &s, const float (&value)[NV], float *out)
     {
         put(s, value, lds);
         __syncthreads();
@@ -300,23 +303,29 @@ template <int VEC, bool WIDE> struct GroupSum {
     }
 };
 // what the groups' table has for the channels of a seat
-template <int VEC, bool WIDE> __device__ __forceinline__ void spread(float (&out)[VEC], const float *table, const Seat &s, const Columns &c, int cg)
+template <int VEC, int UNIT> __device__ __forceinline__ void spread(float (&out)[VEC], const float *table, const Seat &s, const Columns &c, int cg)
 {
-    const int first = s.side * c.groups;
-    if constexpr (WIDE) {
-        const float v = table[first + s.at / cg];
+    const int first = s.side * c.groups, per = cg / UNIT;
+    int g = s.at / cg, r = s.at % cg / UNIT;
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) out[i] = v;
-    } else {
-        int g = s.at / cg, r = s.at % cg;
+    for (int i = 0; i < VEC; i += UNIT) {
+        const float v = table[first + g];
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            out[i] = table[first + g];
-            if (++r == cg) {
-                r = 0;
-                ++g;
-            }
+        for (int j = 0; j < UNIT; ++j) out[i + j] = v;
+        if (i + UNIT < VEC && ++r == per) {
+            r = 0;
+            ++g;
         }
+    }
+}
+// the sums over UNIT neighbours
+template <int VEC, int UNIT> __device__ __forceinline__ void gather(float (&out)[VEC / UNIT], const float (&v)[VEC])
+{
+#pragma unroll
+    for (int i = 0; i < VEC / UNIT; ++i) {
+        out[i] = v[i * UNIT];
+#pragma unroll
+        for (int j = 1; j < UNIT; ++j) out[i] += v[i * UNIT + j];
     }
 }
 
@@ -336,9 +345,9 @@ template <bool BF16, int VEC, int K> struct TileLoad {
 };
 
 // The mean and the sum of squared distances from it, for the groups of a tile: mean[side * groups + group], M2 likewise.
-template <bool BF16, int VEC, int K, bool WIDE>
+template <bool BF16, int VEC, int K, int UNIT>
 __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::raw (&raw)[K], const Seat &s, int64_t first, int positions, const Tiling &t, const Columns &c,
-                                             int cg, float count, GroupSum<VEC, WIDE> &sums, float *mean, float *m2)
+                                             int cg, float count, GroupSum<VEC, UNIT> &sums, float *mean, float *m2)
 {
     using C = Chunk<BF16, VEC>;
     float sum[VEC], m[VEC];
@@ -353,10 +362,12 @@ __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::ra
             for (int v = 0; v < VEC; ++v) sum[v] += x[v];
         }
     }
-    sums(s, sum, mean);
+    float brought[VEC / UNIT];
+    gather<VEC, UNIT>(brought, sum);
+    sums(s, brought, mean);
     for (int q = threadIdx.x; q < t.side * c.groups; q += blockDim.x) mean[q] /= count;
     __syncthreads();
-    spread<VEC, WIDE>(m, mean, s, c, cg);
+    spread<VEC, UNIT>(m, mean, s, c, cg);
 #pragma unroll
     for (int v = 0; v < VEC; ++v) sum[v] = 0.f;
 #pragma unroll
@@ -371,19 +382,20 @@ __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::ra
             }
         }
     }
-    sums(s, sum, m2);
+    gather<VEC, UNIT>(brought, sum);
+    sums(s, brought, m2);
 }
 
 // y from x in registers, with the tables of mean and 1 / deviation
-template <bool BF16, int VEC, int K, bool WIDE>
+template <bool BF16, int VEC, int K, int UNIT>
 __device__ __forceinline__ void tile_out(const typename Chunk<BF16, VEC>::raw (&raw)[K], const NormArgs &a, const Seat &s, int64_t point, int64_t first, const Tiling &t,
                                          const Columns &c, int cg, const float *mean, const float *rstd)
 {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
     float m[VEC], r[VEC], gamma[VEC], beta[VEC];
-    spread<VEC, WIDE>(m, mean, s, c, cg);
-    spread<VEC, WIDE>(r, rstd, s, c, cg);
+    spread<VEC, UNIT>(m, mean, s, c, cg);
+    spread<VEC, UNIT>(r, rstd, s, c, cg);
     read_floats(gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(beta, a.beta, c.first + s.at, 0.f);
 #pragma unroll
@@ -403,21 +415,21 @@ __device__ __forceinline__ void tile_out(const typename Chunk<BF16, VEC>::raw (&
     }
 }
 
-template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds__(1024) norm_tile_forward_kernel(NormArgs a, Tiling t)
+template <bool BF16, int VEC, int K, int UNIT, int MOST> __global__ void __launch_bounds__(MOST) norm_tile_forward_kernel(NormArgs a, Tiling t)
 {
     using L = TileLoad<BF16, VEC, K>;
     extern __shared__ float lds[];
     const int cg = a.shape.channels / a.groups, tile = blockIdx.y;
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
-    GroupSum<VEC, WIDE> sums = {lds, t, c, cg};
-    float *mean = lds + t.threads * (WIDE ? 1 : VEC), *rstd = mean + t.side * c.groups;
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
+    float *mean = lds + t.threads * (VEC / UNIT), *rstd = mean + t.side * c.groups;
     const float count = static_cast<float>(a.shape.positions) * cg;
     for (int64_t n0 = int64_t(blockIdx.x) * t.side; n0 < a.shape.points; n0 += int64_t(gridDim.x) * t.side) {
         const int64_t n = n0 + s.side;
         typename Chunk<BF16, VEC>::raw raw[K];
         L::template load<true>(raw, a.x, min(n, a.shape.points - 1), s.ty, t.down, a.shape.positions, c.first + s.at);
-        tile_moments<BF16, VEC, K, WIDE>(raw, s, s.ty, a.shape.positions, t, c, cg, count, sums, mean, rstd);
+        tile_moments<BF16, VEC, K, UNIT>(raw, s, s.ty, a.shape.positions, t, c, cg, count, sums, mean, rstd);
         for (int q = threadIdx.x; q < t.side * c.groups; q += blockDim.x) {
             rstd[q] = 1.f / sqrtf(rstd[q] / count + a.eps);
             const int64_t point = n0 + q / c.groups;
@@ -427,13 +439,13 @@ template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds_
             }
         }
         __syncthreads();
-        if (s.has && n < a.shape.points) tile_out<BF16, VEC, K, WIDE>(raw, a, s, n, s.ty, t, c, cg, mean, rstd);
+        if (s.has && n < a.shape.points) tile_out<BF16, VEC, K, UNIT>(raw, a, s, n, s.ty, t, c, cg, mean, rstd);
         __syncthreads();                                 // before the tables are another point's
     }
 }
 
 // h and gamma dz of a tile: what the sums and dx are made of.  kept[k] = dz, raw keeps x.
-template <bool BF16, int VEC, int K, bool WIDE>
+template <bool BF16, int VEC, int K, int UNIT>
 __device__ __forceinline__ void tile_slopes(const typename Chunk<BF16, VEC>::raw (&raw)[K], const typename Chunk<BF16, VEC>::raw (&raw_d)[K], float (&dz)[K][VEC],
                                             const NormGradArgs &a, int64_t first, const Tiling &t, const float (&m)[VEC], const float (&r)[VEC],
                                             const float (&gamma)[VEC], const float (&beta)[VEC], float (&s1)[VEC], float (&s2)[VEC])
@@ -482,7 +494,7 @@ __device__ __forceinline__ void tile_dx(const typename Chunk<BF16, VEC>::raw (&r
     }
 }
 // mean and 1 / deviation of a seat's channels, from the tensors
-template <int VEC, bool WIDE> __device__ __forceinline__ void read_stats(float (&m)[VEC], float (&r)[VEC], const NormGradArgs &a, const Seat &s, const Columns &c, int64_t point, int cg)
+template <int VEC, int UNIT> __device__ __forceinline__ void read_stats(float (&m)[VEC], float (&r)[VEC], const NormGradArgs &a, const Seat &s, const Columns &c, int64_t point, int cg)
 {
     const float *mean = a.mean + point * a.groups + c.group, *rstd = a.rstd + point * a.groups + c.group;
     Columns one = c;
@@ -491,12 +503,12 @@ template <int VEC, bool WIDE> __device__ __forceinline__ void read_stats(float (
     seat.side = 0;
     const int within = c.first - c.group * cg;           // a slice of a group begins inside it
     seat.at += within;
-    spread<VEC, WIDE>(m, mean, seat, one, cg);
-    spread<VEC, WIDE>(r, rstd, seat, one, cg);
+    spread<VEC, UNIT>(m, mean, seat, one, cg);
+    spread<VEC, UNIT>(r, rstd, seat, one, cg);
 }
 
 // A workgroup goes through the points of a piece of a run, `side` at a time.
-template <bool BF16, int VEC, int K, bool WIDE>
+template <bool BF16, int VEC, int K, int UNIT>
 __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a, Tiling t, Pieces pieces, float *parts_gamma, float *parts_beta)
 {
     using L = TileLoad<BF16, VEC, K>;
@@ -504,8 +516,8 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
     const int cg = a.shape.channels / a.groups;
     const Columns c = columns_of(a.shape, a.groups, t, blockIdx.y);
     const Seat s = take_seat<VEC>(t, c);
-    GroupSum<VEC, WIDE> sums = {lds, t, c, cg};
-    const int room = t.threads * (WIDE ? 1 : VEC);
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
+    const int room = t.threads * (VEC / UNIT);
     float *A_of = lds + 2 * room, *B_of = A_of + t.side * c.groups;
     const float share = 1.f / (static_cast<float>(a.shape.positions) * cg);
     float gamma[VEC], beta[VEC], sum_gamma[VEC], sum_beta[VEC];
@@ -521,8 +533,8 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
         float dz[K][VEC], m[VEC], r[VEC], s1[VEC], s2[VEC], A[VEC], B[VEC];
         L::template load<true>(raw, a.x, n, s.ty, t.down, a.shape.positions, c.first + s.at);
         L::template load<true>(raw_d, a.dy, n, s.ty, t.down, a.shape.positions, c.first + s.at);
-        read_stats<VEC, WIDE>(m, r, a, s, c, n, cg);
-        tile_slopes<BF16, VEC, K, WIDE>(raw, raw_d, dz, a, s.ty, t, m, r, gamma, beta, s1, s2);
+        read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
+        tile_slopes<BF16, VEC, K, UNIT>(raw, raw_d, dz, a, s.ty, t, m, r, gamma, beta, s1, s2);
         if (live) {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
@@ -536,14 +548,17 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
             s1[v] *= gamma[v];
             s2[v] *= gamma[v];
         }
-        sums.put(s, s1, lds);
-        sums.put(s, s2, lds + room);
+        float brought[VEC / UNIT];
+        gather<VEC, UNIT>(brought, s1);
+        sums.put(s, brought, lds);
+        gather<VEC, UNIT>(brought, s2);
+        sums.put(s, brought, lds + room);
         __syncthreads();
         sums.add(lds, A_of);
         sums.add(lds + room, B_of);
         __syncthreads();
-        spread<VEC, WIDE>(A, A_of, s, c, cg);
-        spread<VEC, WIDE>(B, B_of, s, c, cg);
+        spread<VEC, UNIT>(A, A_of, s, c, cg);
+        spread<VEC, UNIT>(B, B_of, s, c, cg);
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
             A[v] *= share;
@@ -578,28 +593,120 @@ template <typename F> __device__ __forceinline__ void join_parts(const Parts &pa
     for (int g = threadIdx.x / lanes; g < c.groups; g += blockDim.x / lanes) f(g, lane, lanes, first);
 }
 
-template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds__(512) norm_part_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
+// A piece is read in steps of U positions of a thread, each position down from the one before.
+template <bool BF16, int VEC, int U> struct PieceWalk {
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    int64_t first, end;          // the thread's first position, and where the piece ends
+    int down;
+    __device__ __forceinline__ PieceWalk(const Tiling &t, int piece, int ty, int positions)
+        : first(int64_t(piece) * t.down * t.k + ty), end(min(int64_t(piece + 1) * t.down * t.k, int64_t(positions))), down(t.down)
+    {
+    }
+    template <bool ONCE> __device__ __forceinline__ void load(typename C::raw (&raw)[U], const T *from, int64_t stride, int64_t at) const
+    {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const T *p = from + min(at + u * down, end - 1) * stride;
+            raw[u] = ONCE ? C::load_once(p) : C::load(p);
+        }
+    }
+};
+// A chunk of an output that may be an input itself: the columns that the last chunk shares with its neighbour are the neighbour's, which may have replaced
+// them before this thread read them.
+template <bool BF16, int VEC> __device__ __forceinline__ void put_chunk(typename Chunk<BF16, 1>::element *to, const float (&v)[VEC], const Columns &c, const Seat &s)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    const int own = (c.width + VEC - 1) / VEC * VEC - c.width;           // the first element that is the last chunk's alone
+    if (own == 0 || s.at < c.width - VEC) {
+        Chunk<BF16, VEC>::store(to, Chunk<BF16, VEC>::narrow(v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (i >= own) Element<BF16>::put(to + i, v[i]);
+    }
+}
+template <bool BF16> __device__ __forceinline__ auto *channel_of(const Rows &v, int64_t point, int channel)
+{
+    return static_cast<typename Chunk<BF16, 1>::element *>(v.p) + point * v.point_stride + channel;
+}
+
+// A thread's own mean and squared distances first, step by step, then the workgroup's about its mean: sum of (M2 + n (mean - all)^2).
+template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_part_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
+{
+    constexpr int U = 4, NV = VEC / UNIT;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
     const int cg = a.shape.channels / a.groups, tile = blockIdx.y, piece = blockIdx.x % t.pieces;
     const int64_t local = blockIdx.x / t.pieces, n = first_point + local;
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     const int cg_tile = t.slices == 1 ? cg : c.width;    // a slice is all that a tile has of its group
-    GroupSum<VEC, WIDE> sums = {lds, t, c, cg_tile};
-    float *mean = lds + t.threads * (WIDE ? 1 : VEC), *m2 = mean + c.groups;
-    const int64_t begin = int64_t(piece) * t.down * K, first = begin + s.ty;
-    const float count = static_cast<float>(min(int64_t(t.down) * K, a.shape.positions - begin)) * (c.width / c.groups);
-    typename Chunk<BF16, VEC>::raw raw[K];
-    L::template load<false>(raw, a.x, n, first, t.down, a.shape.positions, c.first + s.at);
-    tile_moments<BF16, VEC, K, WIDE>(raw, s, first, a.shape.positions, t, c, cg_tile, count, sums, mean, m2);
-    for (int g = threadIdx.x; g < c.groups; g += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + g] = f2{mean[g], m2[g]};
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg_tile};
+    float *mean_of = lds + t.threads * NV, *m2_of = mean_of + c.groups;
+    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
+    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at);
+    float mean[NV], m2[NV], have = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) mean[i] = m2[i] = 0.f;
+    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+        typename C::raw raw[U];
+        walk.template load<false>(raw, x, a.x.position_stride, p);
+        auto step = [&](auto all) {
+            const int rows = all() ? U : static_cast<int>((walk.end - p + t.down - 1) / t.down);
+            float v[U][VEC], sum[NV], brought[NV];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) sum[i] = 0.f;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                C::widen(raw[u], v[u]);
+                gather<VEC, UNIT>(brought, v[u]);
+#pragma unroll
+                for (int i = 0; i < NV; ++i) sum[i] += all() || u < rows ? brought[i] : 0.f;
+            }
+            const float fresh = static_cast<float>(rows * UNIT), share = 1.f / fresh, total = have + fresh;
+            const float part = fresh / total;
+            const float weight = have * part;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const float m = sum[i] * share, apart = m - mean[i];
+                float q = 0.f;
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+                    if (all() || u < rows) {
+#pragma unroll
+                        for (int j = 0; j < UNIT; ++j) {
+                            const float d = v[u][i * UNIT + j] - m;
+                            q = fmaf(d, d, q);
+                        }
+                    }
+                mean[i] = fmaf(apart, part, mean[i]);
+                m2[i] += fmaf(apart * apart, weight, q);
+            }
+            have = total;
+        };
+        if (p + (U - 1) * t.down < walk.end) step(std::true_type());
+        else step(std::false_type());
+    }
+    float brought[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) brought[i] = have * mean[i];
+    sums(s, brought, mean_of);
+    const int64_t begin = int64_t(piece) * t.down * t.k;
+    const float count = static_cast<float>(walk.end - begin) * (c.width / c.groups);
+    for (int g = threadIdx.x; g < c.groups; g += blockDim.x) mean_of[g] /= count;
+    __syncthreads();
+    float all[VEC];
+    spread<VEC, UNIT>(all, mean_of, s, c, cg_tile);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) brought[i] = have > 0.f ? fmaf(have * (mean[i] - all[i * UNIT]), mean[i] - all[i * UNIT], m2[i]) : 0.f;
+    sums(s, brought, m2_of);
+    for (int g = threadIdx.x; g < c.groups; g += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + g] = f2{mean_of[g], m2_of[g]};
 }
 
-template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds__(512) norm_join_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
+template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_join_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    constexpr int U = 4;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
     const int cg = a.shape.channels / a.groups, tile = blockIdx.y;
     const int piece = t.pieces - 1 - static_cast<int>(blockIdx.x % t.pieces);            // the last ones read are the likeliest in the caches
@@ -607,13 +714,15 @@ template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds_
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     float *mean = lds, *rstd = mean + c.groups;
-    const int64_t first = int64_t(piece) * t.down * K + s.ty;
-    typename Chunk<BF16, VEC>::raw raw[K];
-    L::template load<true>(raw, a.x, n, first, t.down, a.shape.positions, c.first + s.at);
+    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
+    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at);
+    auto *y = channel_of<BF16>(a.y, n, c.first + s.at);
+    typename C::raw raw[U];
+    walk.template load<true>(raw, x, a.x.position_stride, walk.first);                   // on its way while the statistics are joined
     join_parts(parts, t, c, n, tile, [&](int g, int lane, int lanes, int first_tile) {
         // the values of piece i of slice j: rows times columns
         auto values = [&](int i, int j) {
-            const int rows = min(t.down * K, a.shape.positions - i * t.down * K);
+            const int rows = min(t.down * t.k, a.shape.positions - i * t.down * t.k);
             const int columns = t.slices == 1 ? cg : slice_begin(t, cg, j + 1) - slice_begin(t, cg, j);
             return static_cast<double>(rows) * columns;
         };
@@ -639,31 +748,76 @@ template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds_
         }
     });
     __syncthreads();
-    if (s.has) tile_out<BF16, VEC, K, WIDE>(raw, a, s, n, first, t, c, t.slices == 1 ? cg : c.width, mean, rstd);
+    if (!s.has) return;
+    float m[VEC], r[VEC], gamma[VEC], beta[VEC];
+    const int cg_tile = t.slices == 1 ? cg : c.width;
+    spread<VEC, UNIT>(m, mean, s, c, cg_tile);
+    spread<VEC, UNIT>(r, rstd, s, c, cg_tile);
+    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
+    read_floats(beta, a.beta, c.first + s.at, 0.f);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) gamma[v] *= r[v];
+    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+        if (p != walk.first) walk.template load<true>(raw, x, a.x.position_stride, p);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = p + u * t.down;
+            if (at >= walk.end) break;
+            float v[VEC];
+            C::widen(raw[u], v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = fmaf(v[i] - m[i], gamma[i], beta[i]);
+            activate(a.activation, v);
+            put_chunk<BF16, VEC>(y + at * a.y.position_stride, v, c, s);
+        }
+    }
 }
 
-template <bool BF16, int VEC, int K, bool WIDE>
-__global__ void __launch_bounds__(512) norm_part_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point, float *parts_gamma, float *parts_beta)
+template <bool BF16, int VEC, int UNIT>
+__global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point, float *parts_gamma, float *parts_beta)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    constexpr int U = 4, NV = VEC / UNIT;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
     const int cg = a.shape.channels / a.groups, tile = blockIdx.y, piece = blockIdx.x % t.pieces;
     const int64_t local = blockIdx.x / t.pieces, n = first_point + local;
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     const int cg_tile = t.slices == 1 ? cg : c.width;
-    GroupSum<VEC, WIDE> sums = {lds, t, c, cg_tile};
-    const int room = t.threads * (WIDE ? 1 : VEC);
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg_tile};
+    const int room = t.threads * NV;
     float *A_of = lds + 2 * room, *B_of = A_of + c.groups;
-    const int64_t first = int64_t(piece) * t.down * K + s.ty;
-    typename Chunk<BF16, VEC>::raw raw[K], raw_d[K];
-    float dz[K][VEC], m[VEC], r[VEC], s1[VEC], s2[VEC], gamma[VEC], beta[VEC];
-    L::template load<false>(raw, a.x, n, first, t.down, a.shape.positions, c.first + s.at);
-    L::template load<false>(raw_d, a.dy, n, first, t.down, a.shape.positions, c.first + s.at);
+    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
+    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at), *dy = channel_of<BF16>(a.dy, n, c.first + s.at);
+    float m[VEC], r[VEC], s1[VEC], s2[VEC], gamma[VEC], beta[VEC];
     read_floats(gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(beta, a.beta, c.first + s.at, 0.f);
-    read_stats<VEC, WIDE>(m, r, a, s, c, n, cg);
-    tile_slopes<BF16, VEC, K, WIDE>(raw, raw_d, dz, a, first, t, m, r, gamma, beta, s1, s2);
+    read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) s1[v] = s2[v] = 0.f;
+    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+        typename C::raw raw[U], raw_d[U];
+        walk.template load<false>(raw, x, a.x.position_stride, p);
+        walk.template load<false>(raw_d, dy, a.dy.position_stride, p);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (p + u * t.down >= walk.end) break;
+            float h[VEC], z[VEC], d[VEC];
+            C::widen(raw[u], h);
+            C::widen(raw_d[u], d);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                h[v] = (h[v] - m[v]) * r[v];
+                z[v] = fmaf(h[v], gamma[v], beta[v]);
+            }
+            through_slope(a.activation, z, d);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                s1[v] += d[v];
+                s2[v] = fmaf(d[v], h[v], s2[v]);
+            }
+        }
+    }
     if (parts_gamma) {
         auto give = [&](float *to) { return [=](int col, float total) { to[int64_t(blockIdx.x) * a.shape.channels + c.first + col] = total; }; };
         add_columns(s2, s.has, s.at, s.ty, t.down, c.width, lds, give(parts_gamma));
@@ -674,8 +828,11 @@ __global__ void __launch_bounds__(512) norm_part_backward_kernel(NormGradArgs a,
         s1[v] *= gamma[v];
         s2[v] *= gamma[v];
     }
-    sums.put(s, s1, lds);
-    sums.put(s, s2, lds + room);
+    float brought[NV];
+    gather<VEC, UNIT>(brought, s1);
+    sums.put(s, brought, lds);
+    gather<VEC, UNIT>(brought, s2);
+    sums.put(s, brought, lds + room);
     __syncthreads();
     sums.add(lds, A_of);
     sums.add(lds + room, B_of);
@@ -683,9 +840,10 @@ __global__ void __launch_bounds__(512) norm_part_backward_kernel(NormGradArgs a,
     for (int g = threadIdx.x; g < c.groups; g += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + g] = f2{A_of[g], B_of[g]};
 }
 
-template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds__(512) norm_join_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point)
+template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_join_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    constexpr int U = 4;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
     const int cg = a.shape.channels / a.groups, tile = blockIdx.y;
     const int piece = t.pieces - 1 - static_cast<int>(blockIdx.x % t.pieces);
@@ -693,11 +851,12 @@ template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds_
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     float *A_of = lds, *B_of = A_of + c.groups;
-    const int64_t first = int64_t(piece) * t.down * K + s.ty;
-    typename Chunk<BF16, VEC>::raw raw[K], raw_d[K];
-    float dz[K][VEC], m[VEC], r[VEC], s1[VEC], s2[VEC], gamma[VEC], beta[VEC], A[VEC], B[VEC];
-    L::template load<true>(raw, a.x, n, first, t.down, a.shape.positions, c.first + s.at);
-    L::template load<true>(raw_d, a.dy, n, first, t.down, a.shape.positions, c.first + s.at);
+    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
+    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at), *dy = channel_of<BF16>(a.dy, n, c.first + s.at);
+    auto *dx = channel_of<BF16>(a.dx, n, c.first + s.at);
+    typename C::raw raw[U], raw_d[U];
+    walk.template load<true>(raw, x, a.x.position_stride, walk.first);
+    walk.template load<true>(raw_d, dy, a.dy.position_stride, walk.first);
     const double all = static_cast<double>(a.shape.positions) * cg;
     join_parts(parts, t, c, n, tile, [&](int g, int lane, int lanes, int first_tile) {
         double sum_A = 0.0, sum_B = 0.0;
@@ -715,15 +874,38 @@ template <bool BF16, int VEC, int K, bool WIDE> __global__ void __launch_bounds_
             B_of[g] = static_cast<float>(sum_B / all);
         }
     });
+    float m[VEC], r[VEC], gamma[VEC], beta[VEC], A[VEC], B[VEC];
     read_floats(gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(beta, a.beta, c.first + s.at, 0.f);
-    read_stats<VEC, WIDE>(m, r, a, s, c, n, cg);
+    read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
     __syncthreads();
+    if (!s.has) return;
     const int cg_tile = t.slices == 1 ? cg : c.width;
-    spread<VEC, WIDE>(A, A_of, s, c, cg_tile);
-    spread<VEC, WIDE>(B, B_of, s, c, cg_tile);
-    tile_slopes<BF16, VEC, K, WIDE>(raw, raw_d, dz, a, first, t, m, r, gamma, beta, s1, s2);
-    if (s.has) tile_dx<BF16, VEC, K>(raw, dz, a, s, c, n, first, t, m, r, gamma, A, B);
+    spread<VEC, UNIT>(A, A_of, s, c, cg_tile);
+    spread<VEC, UNIT>(B, B_of, s, c, cg_tile);
+    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+        if (p != walk.first) {
+            walk.template load<true>(raw, x, a.x.position_stride, p);
+            walk.template load<true>(raw_d, dy, a.dy.position_stride, p);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = p + u * t.down;
+            if (at >= walk.end) break;
+            float h[VEC], z[VEC], d[VEC];
+            C::widen(raw[u], h);
+            C::widen(raw_d[u], d);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                h[v] = (h[v] - m[v]) * r[v];
+                z[v] = fmaf(h[v], gamma[v], beta[v]);
+            }
+            through_slope(a.activation, z, d);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) d[v] = r[v] * (fmaf(gamma[v], d[v], -A[v]) - h[v] * B[v]);
+            put_chunk<BF16, VEC>(dx + at * a.dx.position_stride, d, c, s);
+        }
+    }
 }
 
 // ---- which of them ----------------------------------------------------------------------------------------------------------------------------
@@ -742,69 +924,78 @@ int across_of(const LayerShape &s, int lanes)
 
 int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
-constexpr int kPartChunks = 8, kPartThreads = 512;       // of norm_part_* and norm_join_*
 constexpr int kMostGroups = 4096;                        // sums of a workgroup: with what they are made from they fit 64 KB of LDS
+constexpr int kPartThreads = 256;                        // of norm_part_* and norm_join_*
+constexpr int kForwardChunks = 8, kForwardThreads = 1024, kBackwardChunks = 4, kBackwardThreads = 512;   // of norm_tile_*
 
-// Tiles in registers: at most `threads` threads with `k` chunks each; k == 0: the point is too large, and is cut into pieces.
+int vec_of(const LayerShape &s) { return s.channels < (s.bf16 ? 8 : 4) ? 1 : s.bf16 ? 8 : 4; }
+int across_for(const LayerShape &s, int groups, int tiles) { return ceil_div(int64_t(ceil_div(groups, tiles)) * (s.channels / groups), vec_of(s)); }
+// Whether the seats of a column can be added up inside a wavefront; rounds `down` for it where there is room.
+void fold_columns(Tiling *t)
+{
+    t->fold = 0;
+    if (t->across > 32 || (t->across & (t->across - 1)) != 0) return;
+    const int step = 64 / t->across, down = (t->down + step - 1) / step * step;
+    if (t->side > 1 ? t->down % step != 0 : down * t->across > t->threads) return;
+    t->down = t->side > 1 ? t->down : down;
+    t->fold = 1;
+}
+
+// Tiles in registers: at most so many threads and chunks of each; k == 0: the point is too large, and is cut into pieces.  Small workgroups, of which
+// several share a compute unit and one loads while others add up; so tiles get narrower (down to a cache line of columns) before they get more threads,
+// and more threads rather than more chunks each where there are few of them.
 Tiling tile(const LayerShape &s, int groups, int most_threads, int most_chunks)
 {
-    const int vec = s.channels < (s.bf16 ? 8 : 4) ? 1 : s.bf16 ? 8 : 4, e = s.bf16 ? 2 : 4, cg = s.channels / groups;
+    const int cg = s.channels / groups, line = std::max(1, 128 / (cg * (s.bf16 ? 2 : 4)));
     Tiling t = {};
-    t.slices = t.unit = 1;
-    t.side = 1;
-    t.pieces = 1;
-    // narrowest tiles: whole groups, a cache line of columns
-    const int least = std::min(groups, std::max(1, 128 / (cg * e)));
-    const int most_tiles = std::max(1, groups / least);
-    auto across_for = [&](int tiles) { return ceil_div(int64_t(ceil_div(groups, tiles)) * cg, vec); };
-    // as few tiles as fit, more where there are few points
-    int tiles = 1;
-    auto fits = [&](int n) {
-        return across_for(n) <= most_threads && ceil_div(groups, n) <= kMostGroups && int64_t(s.positions) <= int64_t(most_threads / across_for(n)) * most_chunks;
+    t.slices = t.unit = t.side = t.pieces = 1;
+    const int most_tiles = std::max(1, groups / line);
+    auto fits = [&](int threads, int chunks, int tiles) {
+        const int across = across_for(s, groups, tiles);
+        return across <= threads && ceil_div(groups, tiles) <= kMostGroups && int64_t(s.positions) <= int64_t(threads / across) * chunks;
     };
-    while (tiles < most_tiles && !fits(tiles)) tiles = std::min(most_tiles, tiles * 2);
-    if (!fits(tiles)) return t;
-    while (tiles < most_tiles && s.points * tiles < kUnits) tiles = std::min(most_tiles, tiles * 2);
-    t.tiles = tiles;
-    t.across = across_for(tiles);
-    // few threads with many chunks each where there are many tiles, else many threads
-    const bool many = s.points * tiles >= 4 * kUnits;
-    t.threads = 256;
-    for (;;) {
-        const int down = t.threads / t.across;
-        if (down > 0 && (int64_t(down) * (many ? most_chunks : 2) >= s.positions || t.threads == most_threads)) break;
-        t.threads *= 2;
+    auto more = [&](int tiles) { return std::min(most_tiles, tiles * 2); };
+    for (t.threads = 256; t.threads <= most_threads; t.threads *= 2) {
+        int tiles = 1;
+        while (tiles < most_tiles && !fits(t.threads, most_chunks, tiles)) tiles = more(tiles);
+        if (!fits(t.threads, most_chunks, tiles)) continue;
+        while (tiles < most_tiles && s.points * tiles < kUnits) tiles = more(tiles);
+        while (t.threads < most_threads && s.points * tiles < 2 * kUnits && !fits(t.threads, 1, tiles)) t.threads *= 2;
+        t.tiles = tiles;
+        t.across = across_for(s, groups, tiles);
+        t.k = 1;
+        while (int64_t(t.threads / t.across) * t.k < s.positions) t.k *= 2;
+        t.down = ceil_div(s.positions, t.k);             // as even as can be
+        t.side = std::max(1, std::min(t.threads / (t.across * t.down), kMostGroups / ceil_div(groups, tiles)));
+        t.side = static_cast<int>(std::min<int64_t>(t.side, std::max<int64_t>(1, s.points)));
+        fold_columns(&t);
+        return t;
     }
-    t.down = std::min(t.threads / t.across, s.positions);
-    t.k = 1;
-    while (int64_t(t.down) * t.k < s.positions) t.k *= 2;
-    t.down = ceil_div(s.positions, t.k);                 // as even as can be
-    t.side = std::max(1, std::min(t.threads / (t.across * t.down), kMostGroups / ceil_div(groups, tiles)));
-    t.side = static_cast<int>(std::min<int64_t>(t.side, std::max<int64_t>(1, s.points)));
     return t;
 }
 Tiling cut(const LayerShape &s, int groups)
 {
-    const int vec = s.channels < (s.bf16 ? 8 : 4) ? 1 : s.bf16 ? 8 : 4, cg = s.channels / groups;
+    const int vec = vec_of(s), cg = s.channels / groups;
     Tiling t = {};
     t.side = t.slices = 1;
     t.threads = kPartThreads;
-    t.k = kPartChunks;
     t.unit = cg % vec == 0 ? vec : 1;
     if (ceil_div(cg, vec) > t.threads) {                 // a group is wider than a workgroup
         t.slices = ceil_div(cg, int64_t(t.threads) * vec);
         t.tiles = groups * t.slices;
         t.across = ceil_div(int64_t(ceil_div(cg / t.unit, t.slices)) * t.unit, vec);
     } else {
-        auto across_for = [&](int tiles) { return ceil_div(int64_t(ceil_div(groups, tiles)) * cg, vec); };
         t.tiles = ceil_div(ceil_div(s.channels, vec), t.threads);
-        while (across_for(t.tiles) > t.threads) ++t.tiles;
-        t.across = across_for(t.tiles);
+        while (across_for(s, groups, t.tiles) > t.threads) ++t.tiles;
+        t.across = across_for(s, groups, t.tiles);
     }
+    // positions of a thread: few where that gives the chip enough workgroups, many where it has enough anyway
     t.down = t.threads / t.across;
+    t.k = 8;
+    while (t.k < 32 && s.points * t.tiles * (int64_t(s.positions) / (int64_t(t.down) * t.k)) > 16 * kUnits) t.k *= 2;
     t.pieces = ceil_div(s.positions, int64_t(t.down) * t.k);
-    t.down = ceil_div(ceil_div(s.positions, t.pieces), t.k);
-    t.pieces = ceil_div(s.positions, int64_t(t.down) * t.k);
+    t.down = std::min(t.down, s.positions);
+    fold_columns(&t);
     return t;
 }
 int most_groups(const Tiling &t, int groups) { return t.slices > 1 ? 1 : ceil_div(groups, t.tiles); }
@@ -826,16 +1017,22 @@ template <typename F> void with_k(int k, F f)
     default: f(std::integral_constant<int, 8>()); break;
     }
 }
-// f(bf16, vec, wide)
+// f(bf16, vec, unit): channels of a load, and of those the neighbours that always lie in one group
 template <typename F> void with_types(const LayerShape &s, int groups, F f)
 {
     using Yes = std::true_type;
     using No = std::false_type;
-    const int vec = s.bf16 ? 8 : 4;
-    const bool wide = s.channels / groups % vec == 0;
-    if (s.channels < vec) s.bf16 ? f(Yes(), std::integral_constant<int, 1>(), No()) : f(No(), std::integral_constant<int, 1>(), No());
-    else if (s.bf16) wide ? f(Yes(), std::integral_constant<int, 8>(), Yes()) : f(Yes(), std::integral_constant<int, 8>(), No());
-    else wide ? f(No(), std::integral_constant<int, 4>(), Yes()) : f(No(), std::integral_constant<int, 4>(), No());
+    const int vec = vec_of(s), cg = s.channels / groups, unit = cg % vec == 0 ? vec : vec % cg == 0 ? cg : 1;
+    auto with = [&](auto bf16, auto v) {
+        constexpr int V = v();
+        if (unit == V) f(bf16, v, std::integral_constant<int, V>());
+        else if (V > 4 && unit == 4) f(bf16, v, std::integral_constant<int, V >= 4 ? 4 : 1>());
+        else if (V > 2 && unit == 2) f(bf16, v, std::integral_constant<int, V >= 2 ? 2 : 1>());
+        else f(bf16, v, std::integral_constant<int, 1>());
+    };
+    if (vec == 1) s.bf16 ? with(Yes(), std::integral_constant<int, 1>()) : with(No(), std::integral_constant<int, 1>());
+    else if (s.bf16) with(Yes(), std::integral_constant<int, 8>());
+    else with(No(), std::integral_constant<int, 4>());
 }
 template <typename F> void with_lanes(int lanes, F f)
 {
@@ -858,7 +1055,6 @@ int64_t rows_of_workgroup(const LayerShape &s, int across, int workgroups_per_un
     length = (length + step - 1) / step * step;
     return std::max<int64_t>({1, length, std::min(step * steps, (s.points + step - 1) / step * step)});
 }
-constexpr int kForwardChunks = 8, kForwardThreads = 1024, kBackwardChunks = 8, kBackwardThreads = 512;
 // points of a piece: a workgroup's sums of the parameters' gradients are over so many that they are little beside what it reads
 int64_t points_of_piece(const LayerShape &s, const Tiling &t)
 {
@@ -896,6 +1092,21 @@ BackwardPlan plan_backward(const LayerShape &s, int groups)
 
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
 
+// What a backward call keeps in its workspace: rows of the pieces' sums for dgamma and dbeta, rows beside them, pairs of sums of the groups.
+struct BackwardRoom {
+    size_t table, beside, pairs;
+    size_t bytes() const { return 2 * table + 2 * beside + pairs; }
+};
+BackwardRoom room_of(const LayerShape &s, int groups, const BackwardPlan &p, const int64_t *bounds, int runs)
+{
+    const int64_t most = most_pieces(bounds, runs, p.units_per_point, p.length), rows = p.cut ? s.points * p.units_per_point : most;
+    BackwardRoom r;
+    r.table = align_up(static_cast<size_t>(rows) * s.channels * sizeof(float));
+    r.beside = align_up(static_cast<size_t>(rows_beside(most, runs)) * s.channels * sizeof(float));
+    r.pairs = p.cut ? static_cast<size_t>(batch_points(s, p.t, 2)) * p.t.tiles * p.t.pieces * most_groups(p.t, groups) * sizeof(f2) : 0;
+    return r;
+}
+
 }  // namespace
 
 size_t norm_forward_bytes(const LayerShape &s, int groups)
@@ -907,12 +1118,7 @@ size_t norm_forward_bytes(const LayerShape &s, int groups)
 
 size_t norm_backward_bytes(const LayerShape &s, int groups, const int64_t *bounds, int runs)
 {
-    if (s.points == 0) return 0;
-    const BackwardPlan p = plan_backward(s, groups);
-    const int64_t rows = p.cut ? s.points * p.units_per_point : most_pieces(bounds, runs, p.units_per_point, p.length);
-    size_t bytes = 2 * align_up(static_cast<size_t>(rows) * s.channels * sizeof(float));
-    if (p.cut) bytes += static_cast<size_t>(batch_points(s, p.t, 2)) * p.t.tiles * p.t.pieces * most_groups(p.t, groups) * sizeof(f2);
-    return bytes;
+    return s.points == 0 ? 0 : room_of(s, groups, plan_backward(s, groups), bounds, runs).bytes();
 }
 
 hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t stream)
@@ -930,11 +1136,11 @@ hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t s
     }
     const Tiling t = tile(s, a.groups, kForwardThreads, kForwardChunks);
     if (t.k) {
-        with_types(s, a.groups, [&](auto bf16, auto vec, auto wide) {
+        with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
             with_k(t.k, [&](auto k) {
                 const dim3 grid(static_cast<unsigned>(std::min<int64_t>((s.points + t.side - 1) / t.side, 1 << 20)), t.tiles);
-                const size_t lds = (t.threads * (wide() ? 1 : vec()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float);
-                norm_tile_forward_kernel<bf16(), vec(), k(), wide()><<<grid, t.threads, lds, stream>>>(a, t);
+                const size_t lds = (t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float);
+                (t.threads > 512 ? norm_tile_forward_kernel<bf16(), vec(), k(), unit(), 1024> : norm_tile_forward_kernel<bf16(), vec(), k(), unit(), 512>)<<<grid, t.threads, lds, stream>>>(a, t);
             });
         });
         return hipGetLastError();
@@ -944,10 +1150,10 @@ hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t s
     const int64_t batch = batch_points(s, c, 1);
     for (int64_t n = 0; n < s.points; n += batch) {
         const dim3 grid(static_cast<unsigned>(std::min(batch, s.points - n) * c.pieces), c.tiles);
-        with_types(s, a.groups, [&](auto bf16, auto vec, auto wide) {
-            const size_t tables = 2 * parts.stride * sizeof(float), lds = c.threads * (wide() ? 1 : vec()) * sizeof(float) + tables;
-            norm_part_forward_kernel<bf16(), vec(), kPartChunks, wide()><<<grid, c.threads, lds, stream>>>(a, c, parts, n);
-            norm_join_forward_kernel<bf16(), vec(), kPartChunks, wide()><<<grid, c.threads, tables, stream>>>(a, c, parts, n);
+        with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
+            const size_t tables = 2 * parts.stride * sizeof(float), lds = c.threads * (vec() / unit()) * sizeof(float) + tables;
+            norm_part_forward_kernel<bf16(), vec(), unit()><<<grid, c.threads, lds, stream>>>(a, c, parts, n);
+            norm_join_forward_kernel<bf16(), vec(), unit()><<<grid, c.threads, tables, stream>>>(a, c, parts, n);
         });
     }
     return hipGetLastError();
@@ -958,42 +1164,43 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
     const LayerShape &s = a.shape;
     const bool sums = a.dgamma || a.dbeta;
     if (!sums && (!a.dx.p || s.points == 0)) return hipSuccess;
-    if (s.points == 0) {                                 // sums of nothing
-        for (int r = 0; r < a.runs; r += Pieces::kRuns) {
-            Pieces p;
-            lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), 1, 1, &p);
-            launch_sum_pieces<true>(nullptr, nullptr, s.channels, p, a.dgamma ? a.dgamma + int64_t(r) * s.channels : nullptr,
-                                    a.dbeta ? a.dbeta + int64_t(r) * s.channels : nullptr, stream);
+    BackwardPlan p = {};
+    p.units_per_point = p.length = 1;
+    float *parts_gamma = nullptr, *parts_beta = nullptr, *beside = nullptr;
+    if (s.points > 0) {
+        p = plan_backward(s, a.groups);
+        const BackwardRoom room = room_of(s, a.groups, p, a.bounds, a.runs);
+        char *at = static_cast<char *>(workspace);
+        if (sums) {
+            parts_gamma = reinterpret_cast<float *>(at);
+            parts_beta = reinterpret_cast<float *>(at + room.table);
+            beside = reinterpret_cast<float *>(at + 2 * room.table);
         }
-        return hipGetLastError();
-    }
-    const BackwardPlan p = plan_backward(s, a.groups);
-    const int64_t rows = p.cut ? s.points * p.units_per_point : most_pieces(a.bounds, a.runs, p.units_per_point, p.length);
-    const size_t table = align_up(static_cast<size_t>(rows) * s.channels * sizeof(float));
-    float *parts_gamma = sums ? static_cast<float *>(workspace) : nullptr;
-    float *parts_beta = sums ? reinterpret_cast<float *>(static_cast<char *>(workspace) + table) : nullptr;
-    if (p.cut) {
-        const Tiling &t = p.t;
-        const Parts parts = {reinterpret_cast<f2 *>(static_cast<char *>(workspace) + 2 * table), most_groups(t, a.groups)};
-        const int64_t batch = batch_points(s, t, 2);
-        for (int64_t n = 0; n < s.points; n += batch) {
-            const dim3 grid(static_cast<unsigned>(std::min(batch, s.points - n) * t.pieces), t.tiles);
-            with_types(s, a.groups, [&](auto bf16, auto vec, auto wide) {
-                const size_t tables = 2 * parts.stride * sizeof(float), room = t.threads * vec() * sizeof(float);
-                const size_t lds = 2 * (wide() ? t.threads * sizeof(float) : room) + tables;
-                float *to_gamma = sums ? parts_gamma + n * t.pieces * s.channels : nullptr, *to_beta = sums ? parts_beta + n * t.pieces * s.channels : nullptr;
-                norm_part_backward_kernel<bf16(), vec(), kPartChunks, wide()><<<grid, t.threads, std::max(lds, room), stream>>>(a, t, parts, n, to_gamma, to_beta);
-                if (a.dx.p) norm_join_backward_kernel<bf16(), vec(), kPartChunks, wide()><<<grid, t.threads, tables, stream>>>(a, t, parts, n);
-            });
+        if (p.cut) {
+            const Tiling &t = p.t;
+            const Parts parts = {reinterpret_cast<f2 *>(at + 2 * room.table + 2 * room.beside), most_groups(t, a.groups)};
+            const int64_t batch = batch_points(s, t, 2);
+            for (int64_t n = 0; n < s.points; n += batch) {
+                const dim3 grid(static_cast<unsigned>(std::min(batch, s.points - n) * t.pieces), t.tiles);
+                with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
+                    const size_t tables = 2 * parts.stride * sizeof(float), columns = t.threads * vec() * sizeof(float);
+                    const size_t lds = std::max(2 * t.threads * (vec() / unit()) * sizeof(float) + tables, columns);
+                    float *to_gamma = sums ? parts_gamma + n * t.pieces * s.channels : nullptr, *to_beta = sums ? parts_beta + n * t.pieces * s.channels : nullptr;
+                    norm_part_backward_kernel<bf16(), vec(), unit()><<<grid, t.threads, lds, stream>>>(a, t, parts, n, to_gamma, to_beta);
+                    if (a.dx.p) norm_join_backward_kernel<bf16(), vec(), unit()><<<grid, t.threads, tables, stream>>>(a, t, parts, n);
+                });
+            }
         }
     }
     for (int r = 0; r < a.runs; r += Pieces::kRuns) {
         Pieces pieces;
         const int count = lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), p.units_per_point, p.length, &pieces);
         const float *from_gamma = parts_gamma, *from_beta = parts_beta;
-        if (p.cut) {                                     // rows of all pieces lie in one table
+        if (p.cut && sums) {                             // rows of all pieces lie in one table
             from_gamma += pieces.first[0] * s.channels;
             from_beta += pieces.first[0] * s.channels;
+        } else if (p.cut) {
+            break;
         } else if (count > 0 && p.lanes) {
             const int across = across_of(s, p.lanes);
             const dim3 grid(ceil_div(s.channels / (s.bf16 ? 8 : 4), across), count);
@@ -1002,17 +1209,18 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
             });
         } else if (count > 0) {
             const Tiling &t = p.t;
-            with_types(s, a.groups, [&](auto bf16, auto vec, auto wide) {
+            with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
                 with_k(t.k, [&](auto k) {
-                    const size_t room = t.threads * vec() * sizeof(float);
-                    const size_t lds = 2 * (wide() ? t.threads * sizeof(float) : room) + 2 * t.side * most_groups(t, a.groups) * sizeof(float);
-                    norm_tile_backward_kernel<bf16(), vec(), k(), wide()><<<dim3(count, t.tiles), t.threads, std::max(lds, room), stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                    constexpr int K = k() < kBackwardChunks ? k() : kBackwardChunks;
+                    const size_t columns = t.threads * vec() * sizeof(float);
+                    const size_t lds = std::max((2 * t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float), columns);
+                    norm_tile_backward_kernel<bf16(), vec(), K, unit()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
                 });
             });
         }
         if (sums)
-            launch_sum_pieces<true>(from_gamma, from_beta, s.channels, pieces, a.dgamma ? a.dgamma + int64_t(r) * s.channels : nullptr,
-                                    a.dbeta ? a.dbeta + int64_t(r) * s.channels : nullptr, stream);
+            launch_sum_pieces(from_gamma, from_beta, s.channels, pieces, beside, a.dgamma ? a.dgamma + int64_t(r) * s.channels : nullptr,
+                              a.dbeta ? a.dbeta + int64_t(r) * s.channels : nullptr, stream);
     }
     return hipGetLastError();
 }

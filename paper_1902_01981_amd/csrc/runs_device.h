@@ -59,37 +59,77 @@ inline int64_t most_pieces(const int64_t *bounds, int runs, int64_t per_point, i
     return most;
 }
 
-#ifdef __HIPCC__
-// out[r][c] = the sum over run r's pieces of parts[piece][c], added up in 64 bits in a fixed order; a workgroup has 64 columns of a run.  TWO: the same of
-// a second table behind the first.
-template <int THREADS, bool TWO>
-__global__ void __launch_bounds__(THREADS) sum_pieces_kernel(const float *parts, const float *parts2, int columns, Pieces p, float *out, float *out2)
+// Rows that sums of a run are made of in a first launch, where runs have so many pieces that one workgroup per 64 columns would be long at it: each
+// run in parts of so many pieces, or 0: one launch does.  2 048 pieces of 512 columns, two tables: 97 us in one launch, 6 in two.
+inline int64_t sum_in_parts(int64_t pieces, int runs)
 {
-    __shared__ double meet[TWO ? 2 : 1][THREADS / 64][64];
-    const int r = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane, at = min(c, columns - 1);
-    double sum = 0.0, sum2 = 0.0;
-    for (int i = p.piece[r] + wave; i < p.piece[r + 1]; i += THREADS / 64) {
-        sum += parts[int64_t(i) * columns + at];
-        if constexpr (TWO) sum2 += parts2[int64_t(i) * columns + at];
-    }
-    meet[0][wave][lane] = sum;
-    if constexpr (TWO) meet[1][wave][lane] = sum2;
-    __syncthreads();
-    if (wave == 0 && c < columns) {
-        for (int w = 1; w < THREADS / 64; ++w) sum += meet[0][w][lane];
-        if (out) out[int64_t(r) * columns + c] = static_cast<float>(sum);
-        if constexpr (TWO) {
-            for (int w = 1; w < THREADS / 64; ++w) sum2 += meet[1][w][lane];
-            if (out2) out2[int64_t(r) * columns + c] = static_cast<float>(sum2);
-        }
-    }
+    int64_t length = 64;
+    while (length * length < pieces) length *= 2;
+    return pieces > 64 * int64_t(runs) ? length : 0;
 }
-template <bool TWO> void launch_sum_pieces(const float *parts, const float *parts2, int columns, const Pieces &p, float *out, float *out2, hipStream_t stream)
+// Rows of floats that the sums of any batch of at most `pieces` pieces need beside them, per table.
+inline int64_t rows_beside(int64_t pieces, int runs) { return pieces / 64 + std::min(runs, Pieces::kRuns); }
+
+#ifdef __HIPCC__
+// Sums of rows [begin, end) of a table with so many columns, a workgroup per 64 columns, in a fixed order; for the first wavefront.
+template <int THREADS> __device__ __forceinline__ double sum_rows(const float *table, int64_t columns, int64_t begin, int64_t end, double (*meet)[64])
 {
-    const dim3 grid((columns + 63) / 64, p.runs);
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t at = min(int64_t(blockIdx.x) * 64 + lane, columns - 1);
+    constexpr int WAVES = THREADS / 64, U = 4;
+    double sum = 0.0;
+    for (int64_t i = begin + wave; i < end; i += U * WAVES) {
+        float v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) v[u] = table[min(i + u * WAVES, end - 1) * columns + at];
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum += i + u * WAVES < end ? v[u] : 0.f;
+    }
+    meet[wave][lane] = sum;
+    __syncthreads();
+    if (wave == 0)
+        for (int w = 1; w < WAVES; ++w) sum += meet[w][lane];
+    __syncthreads();
+    return sum;
+}
+// out[r][c] = the sum over run r's pieces of parts[piece][c]; blockIdx.z: of one or the other table
+template <int THREADS> __global__ void __launch_bounds__(THREADS) sum_pieces_kernel(const float *parts, const float *parts2, int columns, Pieces p, float *out, float *out2)
+{
+    __shared__ double meet[THREADS / 64][64];
+    const int r = blockIdx.y, c = blockIdx.x * 64 + threadIdx.x % 64;
+    float *to = blockIdx.z ? out2 : out;
+    if (!to) return;
+    const double sum = sum_rows<THREADS>(blockIdx.z ? parts2 : parts, columns, p.piece[r], p.piece[r + 1], meet);
+    if (threadIdx.x < 64 && c < columns) to[int64_t(r) * columns + c] = static_cast<float>(sum);
+}
+// the same of a run's parts: piece q of `p` is rows of the tables, its sum goes to row q of the others
+static __global__ void __launch_bounds__(256) sum_parts_kernel(const float *parts, const float *parts2, int columns, Pieces p, float *out, float *out2)
+{
+    __shared__ double meet[4][64];
+    const int c = blockIdx.x * 64 + threadIdx.x % 64;
+    const Piece q = find_piece(p, blockIdx.y);
+    const double sum = sum_rows<256>(blockIdx.z ? parts2 : parts, columns, q.begin, q.end, meet);
+    if (threadIdx.x < 64 && c < columns) (blockIdx.z ? out2 : out)[int64_t(blockIdx.y) * columns + c] = static_cast<float>(sum);
+}
+// The sums of a batch's runs, of one table or two; `beside` holds rows_beside rows per table.
+inline void launch_sum_pieces(const float *parts, const float *parts2, int columns, const Pieces &pieces, float *beside, float *out, float *out2, hipStream_t stream)
+{
+    Pieces p = pieces;
+    const unsigned tables = parts2 || out2 ? 2 : 1;
+    const unsigned across = (columns + 63) / 64;
+    if (const int64_t length = sum_in_parts(p.piece[p.runs], p.runs)) {
+        int64_t bounds[Pieces::kRuns + 1];
+        for (int r = 0; r <= p.runs; ++r) bounds[r] = pieces.piece[r];
+        const int count = lay_out_pieces(bounds, p.runs, 1, length, &p);
+        float *beside2 = beside + int64_t(count) * columns;
+        sum_parts_kernel<<<dim3(across, count, tables), 256, 0, stream>>>(parts, parts2, columns, p, beside, beside2);
+        parts = beside;
+        parts2 = beside2;
+    }
+    const dim3 grid(across, p.runs, tables);
     // as many wavefronts as there are pieces to share out
-    if (p.piece[p.runs] >= 16 * p.runs) sum_pieces_kernel<1024, TWO><<<grid, 1024, 0, stream>>>(parts, parts2, columns, p, out, out2);
-    else sum_pieces_kernel<256, TWO><<<grid, 256, 0, stream>>>(parts, parts2, columns, p, out, out2);
+    if (p.piece[p.runs] > 16 * p.runs) sum_pieces_kernel<1024><<<grid, 1024, 0, stream>>>(parts, parts2, columns, p, out, out2);
+    else sum_pieces_kernel<256><<<grid, 256, 0, stream>>>(parts, parts2, columns, p, out, out2);
 }
 #endif
 

@@ -16,29 +16,28 @@ namespace {
 constexpr int kUnits = 256;
 
 // act(z), and d act'(z) from d and z
-template <int VEC> __device__ __forceinline__ void activate(int kind, float (&z)[VEC])
+template <int ACT> __device__ __forceinline__ float activated(float z)
 {
-    if (kind == 1) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) z[v] = z[v] < 0.f ? 0.f : z[v];
-    } else if (kind == 2) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) z[v] = z[v] * __builtin_amdgcn_rcpf(1.f + __expf(-z[v]));
-    }
+    if constexpr (ACT == 1) return z < 0.f ? 0.f : z;
+    if constexpr (ACT == 2) return z * __builtin_amdgcn_rcpf(1.f + __expf(-z));
+    return z;
 }
-template <int VEC> __device__ __forceinline__ void through_slope(int kind, const float (&z)[VEC], float (&d)[VEC])
+template <int ACT> __device__ __forceinline__ float through_slope(float z, float d)
 {
-    if (kind == 1) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) d[v] = z[v] > 0.f ? d[v] : z[v] <= 0.f ? 0.f : z[v];                // not 0 where z is not a number
-    } else if (kind == 2) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z[v]));
-            d[v] *= s * fmaf(z[v], 1.f - s, 1.f);
-        }
+    if constexpr (ACT == 1) return z > 0.f ? d : z <= 0.f ? 0.f : z;     // not 0 where z is not a number
+    if constexpr (ACT == 2) {
+        const float s = __builtin_amdgcn_rcpf(1.f + __expf(-z));
+        return d * (s * fmaf(z, 1.f - s, 1.f));
     }
+    return d;
 }
+// (x - mean) rstd.  From bf16 by one multiply-add: mean rstd is then rounded by itself, which is what the mean's own rounding does to all values of a
+// group anyway, and x has no bits that it would cost.
+template <bool BF16> struct Normal {
+    float scale, shift;
+    __device__ __forceinline__ Normal(float mean, float rstd) : scale(rstd), shift(BF16 ? -mean * rstd : mean) {}
+    __device__ __forceinline__ float operator()(float x) const { return BF16 ? fmaf(x, scale, shift) : (x - shift) * scale; }
+};
 template <int VEC> __device__ __forceinline__ void read_floats(float (&out)[VEC], const float *p, int at, float otherwise)
 {
 #pragma unroll
@@ -47,7 +46,7 @@ template <int VEC> __device__ __forceinline__ void read_floats(float (&out)[VEC]
 
 // ---- points of one position, groups of a few lanes ---------------------------------------------------------------------------------------
 // A thread stays with its chunk and goes through the points, U at a time.  Its group is the LANES lanes around it.
-template <bool BF16, int LANES> __global__ void __launch_bounds__(256) norm_rows_forward_kernel(NormArgs a, int across, int64_t length)
+template <bool BF16, int LANES, int ACT> __global__ void __launch_bounds__(256) norm_rows_forward_kernel(NormArgs a, int across, int64_t length)
 {
     constexpr int VEC = BF16 ? 8 : 4, U = 4;
     using C = Chunk<BF16, VEC>;
@@ -84,8 +83,7 @@ template <bool BF16, int LANES> __global__ void __launch_bounds__(256) norm_rows
             const float rstd = 1.f / sqrtf(fmaf(lanes_total<LANES>(sum), share, a.eps));
             if (n >= end) continue;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = fmaf(v[i] * rstd, gamma[i], beta[i]);
-            activate(a.activation, v);
+            for (int i = 0; i < VEC; ++i) v[i] = activated<ACT>(fmaf(v[i] * rstd, gamma[i], beta[i]));
             C::store(y + n * a.y.point_stride, C::narrow(v));
             if (a.mean && q % LANES == 0) {
                 a.mean[n * a.groups + q / LANES] = mean;
@@ -124,7 +122,7 @@ template <int VEC, typename F> __device__ __forceinline__ void add_columns(const
     __syncthreads();
 }
 
-template <bool BF16, int LANES>
+template <bool BF16, int LANES, int ACT>
 __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a, int across, Pieces pieces, float *parts_gamma, float *parts_beta)
 {
     constexpr int VEC = BF16 ? 8 : 4, U = 4;
@@ -158,17 +156,14 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t n = n0 + u * down;
-                float h[VEC], d[VEC], z[VEC], A = 0.f, B = 0.f;
+                const Normal<BF16> normal(mean[u], rstd[u]);
+                float h[VEC], d[VEC], A = 0.f, B = 0.f;
                 C::widen(raw[u], h);
                 C::widen(raw_d[u], d);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    h[i] = (h[i] - mean[u]) * rstd[u];
-                    z[i] = fmaf(h[i], gamma[i], beta[i]);
-                }
-                through_slope(a.activation, z, d);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
+                    h[i] = normal(h[i]);
+                    d[i] = through_slope<ACT>(fmaf(h[i], gamma[i], beta[i]), d[i]);
                     const float t = gamma[i] * d[i];
                     A += t;
                     B = fmaf(t, h[i], B);
@@ -180,7 +175,7 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
                 for (int i = 0; i < VEC; ++i) {
                     sum_beta[i] += d[i];
                     sum_gamma[i] = fmaf(d[i], h[i], sum_gamma[i]);
-                    d[i] = rstd[u] * (fmaf(gamma[i], d[i], -A) - h[i] * B);
+                    d[i] = rstd[u] * fmaf(-h[i], B, fmaf(gamma[i], d[i], -A));
                 }
                 if (a.dx.p) C::store(dx + n * a.dx.point_stride, C::narrow(d));
             }
@@ -329,107 +324,102 @@ template <int VEC, int UNIT> __device__ __forceinline__ void gather(float (&out)
     }
 }
 
-template <bool BF16, int VEC, int K> struct TileLoad {
+// A thread's chunks of a tensor: positions first, first + down, ... of a point, from one channel on.  Their addresses are a scalar that moves on from one to
+// the next and the thread's own offset.
+template <bool BF16, int VEC> struct Walk {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
-    // positions first + ty + k down of a point (past the last one: the last one, not counted), the chunk at channel `channel`
-    template <bool ONCE> static __device__ __forceinline__ void load(typename C::raw (&raw)[K], const Rows &v, int64_t point, int64_t first, int down, int positions, int channel)
+    T *base;
+    int64_t offset, step;
+    __device__ __forceinline__ Walk(const Rows &v, int64_t point, int64_t first, int channel, int down)
+        : base(static_cast<T *>(v.p)), offset(point * v.point_stride + first * v.position_stride + channel), step(down * v.position_stride)
     {
-        const T *p = static_cast<const T *>(v.p) + point * v.point_stride + channel;
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const T *at = p + min(first + k * down, int64_t(positions - 1)) * v.position_stride;
-            raw[k] = ONCE ? C::load_once(at) : C::load(at);
-        }
     }
+    __device__ __forceinline__ T *at(int k) const { return scalar(base + k * step) + offset; }
+    __device__ __forceinline__ void advance(int k) { base += k * step; }
 };
+// positions of a thread that exist: of K from `first` on, `down` apart
+__device__ __forceinline__ bool exists(int first, int k, int down, int positions) { return static_cast<unsigned>(first + k * down) < static_cast<unsigned>(positions); }
 
 // The mean and the sum of squared distances from it, for the groups of a tile: mean[side * groups + group], M2 likewise.
 template <bool BF16, int VEC, int K, int UNIT>
-__device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::raw (&raw)[K], const Seat &s, int64_t first, int positions, const Tiling &t, const Columns &c,
-                                             int cg, float count, GroupSum<VEC, UNIT> &sums, float *mean, float *m2)
+__device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::raw (&raw)[K], const Seat &s, int positions, const Tiling &t, const Columns &c, int cg,
+                                             float count, GroupSum<VEC, UNIT> &sums, float *mean, float *m2)
 {
     using C = Chunk<BF16, VEC>;
-    float sum[VEC], m[VEC];
+    constexpr int NV = VEC / UNIT;
+    float sum[NV], m[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sum[v] = 0.f;
+    for (int i = 0; i < NV; ++i) sum[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (first + k * t.down < positions) {
+        if (exists(s.ty, k, t.down, positions)) {
             float x[VEC];
             C::widen(raw[k], x);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) sum[v] += x[v];
+            for (int v = 0; v < VEC; ++v) sum[v / UNIT] += x[v];
         }
     }
-    float brought[VEC / UNIT];
-    gather<VEC, UNIT>(brought, sum);
-    sums(s, brought, mean);
+    sums(s, sum, mean);
     for (int q = threadIdx.x; q < t.side * c.groups; q += blockDim.x) mean[q] /= count;
     __syncthreads();
     spread<VEC, UNIT>(m, mean, s, c, cg);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) sum[v] = 0.f;
+    for (int i = 0; i < NV; ++i) sum[i] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (first + k * t.down < positions) {
+        if (exists(s.ty, k, t.down, positions)) {
             float x[VEC];
             C::widen(raw[k], x);
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 x[v] -= m[v];
-                sum[v] = fmaf(x[v], x[v], sum[v]);
+                sum[v / UNIT] = fmaf(x[v], x[v], sum[v / UNIT]);
             }
         }
     }
-    gather<VEC, UNIT>(brought, sum);
-    sums(s, brought, m2);
+    sums(s, sum, m2);
 }
 
-// y from x in registers, with the tables of mean and 1 / deviation
-template <bool BF16, int VEC, int K, int UNIT>
-__device__ __forceinline__ void tile_out(const typename Chunk<BF16, VEC>::raw (&raw)[K], const NormArgs &a, const Seat &s, int64_t point, int64_t first, const Tiling &t,
-                                         const Columns &c, int cg, const float *mean, const float *rstd)
-{
-    using C = Chunk<BF16, VEC>;
-    using T = typename C::element;
-    float m[VEC], r[VEC], gamma[VEC], beta[VEC];
-    spread<VEC, UNIT>(m, mean, s, c, cg);
-    spread<VEC, UNIT>(r, rstd, s, c, cg);
-    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
-    read_floats(beta, a.beta, c.first + s.at, 0.f);
+// y from x: gamma h + beta and the activation; by one multiply-add from bf16, as Normal
+template <bool BF16, int VEC, int ACT> struct Finish {
+    float shift[VEC], scale[VEC], beta[VEC];
+    __device__ __forceinline__ Finish(const NormArgs &a, int channel, const float (&mean)[VEC], const float (&rstd)[VEC])
+    {
+        read_floats(scale, a.gamma, channel, 1.f);
+        read_floats(beta, a.beta, channel, 0.f);
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) gamma[v] *= r[v];
-    T *y = static_cast<T *>(a.y.p) + point * a.y.point_stride + c.first + s.at;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t p = first + k * t.down;
-        if (p < a.shape.positions) {
-            float x[VEC];
-            C::widen(raw[k], x);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) x[v] = fmaf(x[v] - m[v], gamma[v], beta[v]);
-            activate(a.activation, x);
-            C::store(y + p * a.y.position_stride, C::narrow(x));
+        for (int v = 0; v < VEC; ++v) {
+            scale[v] *= rstd[v];
+            shift[v] = mean[v];
+            if (BF16) beta[v] = fmaf(-mean[v], scale[v], beta[v]);
         }
     }
-}
+    __device__ __forceinline__ void operator()(float (&x)[VEC]) const
+    {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) x[v] = activated<ACT>(fmaf(BF16 ? x[v] : x[v] - shift[v], scale[v], beta[v]));
+    }
+};
 
-template <bool BF16, int VEC, int K, int UNIT, int MOST> __global__ void __launch_bounds__(MOST) norm_tile_forward_kernel(NormArgs a, Tiling t)
+template <bool BF16, int VEC, int K, int UNIT, int ACT, int MOST> __global__ void __launch_bounds__(MOST) norm_tile_forward_kernel(NormArgs a, Tiling t)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
-    const int cg = a.shape.channels / a.groups, tile = blockIdx.y;
+    const int cg = a.shape.channels / a.groups, tile = blockIdx.y, positions = a.shape.positions;
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
     float *mean = lds + t.threads * (VEC / UNIT), *rstd = mean + t.side * c.groups;
-    const float count = static_cast<float>(a.shape.positions) * cg;
+    const float count = static_cast<float>(positions) * cg;
     for (int64_t n0 = int64_t(blockIdx.x) * t.side; n0 < a.shape.points; n0 += int64_t(gridDim.x) * t.side) {
         const int64_t n = n0 + s.side;
-        typename Chunk<BF16, VEC>::raw raw[K];
-        L::template load<true>(raw, a.x, min(n, a.shape.points - 1), s.ty, t.down, a.shape.positions, c.first + s.at);
-        tile_moments<BF16, VEC, K, UNIT>(raw, s, s.ty, a.shape.positions, t, c, cg, count, sums, mean, rstd);
+        typename C::raw raw[K];
+        const Walk<BF16, VEC> x(a.x, min(n, a.shape.points - 1), s.ty, c.first + s.at, t.down);
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (exists(s.ty, k, t.down, positions)) raw[k] = C::load_once(x.at(k));
+        tile_moments<BF16, VEC, K, UNIT>(raw, s, positions, t, c, cg, count, sums, mean, rstd);
         for (int q = threadIdx.x; q < t.side * c.groups; q += blockDim.x) {
             rstd[q] = 1.f / sqrtf(rstd[q] / count + a.eps);
             const int64_t point = n0 + q / c.groups;
@@ -439,60 +429,56 @@ template <bool BF16, int VEC, int K, int UNIT, int MOST> __global__ void __launc
             }
         }
         __syncthreads();
-        if (s.has && n < a.shape.points) tile_out<BF16, VEC, K, UNIT>(raw, a, s, n, s.ty, t, c, cg, mean, rstd);
+        if (s.has && n < a.shape.points) {
+            float m[VEC], r[VEC];
+            spread<VEC, UNIT>(m, mean, s, c, cg);
+            spread<VEC, UNIT>(r, rstd, s, c, cg);
+            const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+            const Walk<BF16, VEC> y(a.y, n, s.ty, c.first + s.at, t.down);
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (exists(s.ty, k, t.down, positions)) {
+                    float v[VEC];
+                    C::widen(raw[k], v);
+                    finish(v);
+                    C::store(y.at(k), C::narrow(v));
+                }
+            }
+        }
         __syncthreads();                                 // before the tables are another point's
     }
 }
 
-// h and gamma dz of a tile: what the sums and dx are made of.  kept[k] = dz, raw keeps x.
-template <bool BF16, int VEC, int K, int UNIT>
-__device__ __forceinline__ void tile_slopes(const typename Chunk<BF16, VEC>::raw (&raw)[K], const typename Chunk<BF16, VEC>::raw (&raw_d)[K], float (&dz)[K][VEC],
-                                            const NormGradArgs &a, int64_t first, const Tiling &t, const float (&m)[VEC], const float (&r)[VEC],
-                                            const float (&gamma)[VEC], const float (&beta)[VEC], float (&s1)[VEC], float (&s2)[VEC])
-{
-    using C = Chunk<BF16, VEC>;
+// What a thread needs of its channels for the gradient.
+template <bool BF16, int VEC, int ACT> struct Gradient {
+    float mean[VEC], rstd[VEC], gamma[VEC], beta[VEC];
+    __device__ __forceinline__ float h(float x, int v) const { return Normal<BF16>(mean[v], rstd[v])(x); }
+    // dz from dy; h is left in x
+    __device__ __forceinline__ void slopes(float (&x)[VEC], float (&d)[VEC]) const
+    {
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) s1[v] = s2[v] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        if (first + k * t.down < a.shape.positions) {
-            float h[VEC], z[VEC];
-            C::widen(raw[k], h);
-            C::widen(raw_d[k], dz[k]);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                h[v] = (h[v] - m[v]) * r[v];
-                z[v] = fmaf(h[v], gamma[v], beta[v]);
-            }
-            through_slope(a.activation, z, dz[k]);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                s1[v] += dz[k][v];
-                s2[v] = fmaf(dz[k][v], h[v], s2[v]);
-            }
+        for (int v = 0; v < VEC; ++v) {
+            x[v] = h(x[v], v);
+            d[v] = through_slope<ACT>(fmaf(x[v], gamma[v], beta[v]), d[v]);
         }
     }
-}
-template <bool BF16, int VEC, int K>
-__device__ __forceinline__ void tile_dx(const typename Chunk<BF16, VEC>::raw (&raw)[K], const float (&dz)[K][VEC], const NormGradArgs &a, const Seat &s, const Columns &c,
-                                        int64_t point, int64_t first, const Tiling &t, const float (&m)[VEC], const float (&r)[VEC], const float (&gamma)[VEC],
-                                        const float (&A)[VEC], const float (&B)[VEC])
-{
-    using C = Chunk<BF16, VEC>;
-    using T = typename C::element;
-    T *dx = static_cast<T *>(a.dx.p) + point * a.dx.point_stride + c.first + s.at;
+};
+// dx = rstd (gamma dz - A - h B); where a group is one value gamma dz and A are the same, and nothing is left of them
+template <int VEC> struct Correction {
+    float A[VEC], B[VEC];
+    __device__ __forceinline__ Correction(const float (&sum_A)[VEC], const float (&sum_B)[VEC], float share)
+    {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int64_t p = first + k * t.down;
-        if (p < a.shape.positions) {
-            float h[VEC];
-            C::widen(raw[k], h);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) h[v] = r[v] * (fmaf(gamma[v], dz[k][v], -A[v]) - (h[v] - m[v]) * r[v] * B[v]);
-            C::store(dx + p * a.dx.position_stride, C::narrow(h));
+        for (int v = 0; v < VEC; ++v) {
+            A[v] = sum_A[v] * share;
+            B[v] = sum_B[v] * share;
         }
     }
-}
+    template <typename G> __device__ __forceinline__ float operator()(const G &g, float h, float dz, int v) const
+    {
+        return g.rstd[v] * fmaf(-h, B[v], fmaf(g.gamma[v], dz, -A[v]));
+    }
+};
 // mean and 1 / deviation of a seat's channels, from the tensors
 template <int VEC, int UNIT> __device__ __forceinline__ void read_stats(float (&m)[VEC], float (&r)[VEC], const NormGradArgs &a, const Seat &s, const Columns &c, int64_t point, int cg)
 {
@@ -507,34 +493,75 @@ template <int VEC, int UNIT> __device__ __forceinline__ void read_stats(float (&
     spread<VEC, UNIT>(r, rstd, seat, one, cg);
 }
 
+// The groups' sums of gamma s1 and gamma s2, for every thread.
+template <int VEC, int UNIT>
+__device__ __forceinline__ void bring(GroupSum<VEC, UNIT> &sums, const Seat &s, const float (&gamma)[VEC], float (&s1)[VEC], float (&s2)[VEC], int room, float *A_of, float *B_of)
+{
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+        s1[v] *= gamma[v];
+        s2[v] *= gamma[v];
+    }
+    float brought[VEC / UNIT];
+    gather<VEC, UNIT>(brought, s1);
+    sums.put(s, brought, sums.lds);
+    gather<VEC, UNIT>(brought, s2);
+    sums.put(s, brought, sums.lds + room);
+    __syncthreads();
+    sums.add(sums.lds, A_of);
+    sums.add(sums.lds + room, B_of);
+    __syncthreads();
+}
 // A workgroup goes through the points of a piece of a run, `side` at a time.
-template <bool BF16, int VEC, int K, int UNIT>
+template <bool BF16, int VEC, int K, int UNIT, int ACT>
 __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a, Tiling t, Pieces pieces, float *parts_gamma, float *parts_beta)
 {
-    using L = TileLoad<BF16, VEC, K>;
+    using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
-    const int cg = a.shape.channels / a.groups;
+    const int cg = a.shape.channels / a.groups, positions = a.shape.positions;
     const Columns c = columns_of(a.shape, a.groups, t, blockIdx.y);
     const Seat s = take_seat<VEC>(t, c);
     GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
     const int room = t.threads * (VEC / UNIT);
     float *A_of = lds + 2 * room, *B_of = A_of + t.side * c.groups;
-    const float share = 1.f / (static_cast<float>(a.shape.positions) * cg);
-    float gamma[VEC], beta[VEC], sum_gamma[VEC], sum_beta[VEC];
-    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
-    read_floats(beta, a.beta, c.first + s.at, 0.f);
+    const float share = 1.f / (static_cast<float>(positions) * cg);
+    Gradient<BF16, VEC, ACT> g;
+    float sum_gamma[VEC], sum_beta[VEC];
+    read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
+    read_floats(g.beta, a.beta, c.first + s.at, 0.f);
 #pragma unroll
     for (int v = 0; v < VEC; ++v) sum_gamma[v] = sum_beta[v] = 0.f;
     const Piece piece = find_piece(pieces, blockIdx.x);
     for (int64_t n0 = piece.begin; n0 < piece.end; n0 += t.side) {
         const int64_t n = min(n0 + s.side, piece.end - 1);
         const bool live = s.has && n0 + s.side < piece.end;
-        typename Chunk<BF16, VEC>::raw raw[K], raw_d[K];
-        float dz[K][VEC], m[VEC], r[VEC], s1[VEC], s2[VEC], A[VEC], B[VEC];
-        L::template load<true>(raw, a.x, n, s.ty, t.down, a.shape.positions, c.first + s.at);
-        L::template load<true>(raw_d, a.dy, n, s.ty, t.down, a.shape.positions, c.first + s.at);
-        read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
-        tile_slopes<BF16, VEC, K, UNIT>(raw, raw_d, dz, a, s.ty, t, m, r, gamma, beta, s1, s2);
+        typename C::raw raw[K], raw_d[K];
+        const Walk<BF16, VEC> x(a.x, n, s.ty, c.first + s.at, t.down), dy(a.dy, n, s.ty, c.first + s.at, t.down);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (exists(s.ty, k, t.down, positions)) {
+                raw[k] = C::load_once(x.at(k));
+                raw_d[k] = C::load_once(dy.at(k));
+            }
+        }
+        read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, n, cg);
+        float dz[K][VEC], s1[VEC], s2[VEC];
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) s1[v] = s2[v] = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (exists(s.ty, k, t.down, positions)) {
+                float h[VEC];
+                C::widen(raw[k], h);
+                C::widen(raw_d[k], dz[k]);
+                g.slopes(h, dz[k]);
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) {
+                    s1[v] += dz[k][v];
+                    s2[v] = fmaf(dz[k][v], h[v], s2[v]);
+                }
+            }
+        }
         if (live) {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
@@ -543,28 +570,24 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
             }
         }
         if (!a.dx.p) continue;
+        bring<VEC, UNIT>(sums, s, g.gamma, s1, s2, room, A_of, B_of);
+        if (live) {
+            float A[VEC], B[VEC];
+            spread<VEC, UNIT>(A, A_of, s, c, cg);
+            spread<VEC, UNIT>(B, B_of, s, c, cg);
+            const Correction<VEC> dx_of(A, B, share);
+            const Walk<BF16, VEC> dx(a.dx, n, s.ty, c.first + s.at, t.down);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            s1[v] *= gamma[v];
-            s2[v] *= gamma[v];
-        }
-        float brought[VEC / UNIT];
-        gather<VEC, UNIT>(brought, s1);
-        sums.put(s, brought, lds);
-        gather<VEC, UNIT>(brought, s2);
-        sums.put(s, brought, lds + room);
-        __syncthreads();
-        sums.add(lds, A_of);
-        sums.add(lds + room, B_of);
-        __syncthreads();
-        spread<VEC, UNIT>(A, A_of, s, c, cg);
-        spread<VEC, UNIT>(B, B_of, s, c, cg);
+            for (int k = 0; k < K; ++k) {
+                if (exists(s.ty, k, t.down, positions)) {
+                    float h[VEC];
+                    C::widen(raw[k], h);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-            A[v] *= share;
-            B[v] *= share;
+                    for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, g.h(h[v], v), dz[k][v], v);
+                    C::store(dx.at(k), C::narrow(h));
+                }
+            }
         }
-        if (live) tile_dx<BF16, VEC, K>(raw, dz, a, s, c, n, s.ty, t, m, r, gamma, A, B);
         // the next step's sums are put where this one's were read before the last barrier, and its results written after another one
     }
     if (!parts_gamma) return;
@@ -593,25 +616,22 @@ template <typename F> __device__ __forceinline__ void join_parts(const Parts &pa
     for (int g = threadIdx.x / lanes; g < c.groups; g += blockDim.x / lanes) f(g, lane, lanes, first);
 }
 
-// A piece is read in steps of U positions of a thread, each position down from the one before.
-template <bool BF16, int VEC, int U> struct PieceWalk {
-    using C = Chunk<BF16, VEC>;
-    using T = typename C::element;
-    int64_t first, end;          // the thread's first position, and where the piece ends
-    int down;
-    __device__ __forceinline__ PieceWalk(const Tiling &t, int piece, int ty, int positions)
-        : first(int64_t(piece) * t.down * t.k + ty), end(min(int64_t(piece + 1) * t.down * t.k, int64_t(positions))), down(t.down)
-    {
-    }
-    template <bool ONCE> __device__ __forceinline__ void load(typename C::raw (&raw)[U], const T *from, int64_t stride, int64_t at) const
-    {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const T *p = from + min(at + u * down, end - 1) * stride;
-            raw[u] = ONCE ? C::load_once(p) : C::load(p);
-        }
-    }
+// A thread's positions of a piece: from `first` on, `down` apart, `left` of them; they are taken U at a time.
+struct Stretch {
+    int64_t first;
+    int left;
 };
+__device__ __forceinline__ Stretch stretch_of(const Tiling &t, int piece, int ty, int positions)
+{
+    const int64_t begin = int64_t(piece) * t.down * t.k, end = min(begin + int64_t(t.down) * t.k, int64_t(positions));
+    return {begin + ty, static_cast<int>((end - begin - ty + t.down - 1) / t.down)};     // none, or fewer, where ty is past the end
+}
+template <bool ONCE, bool BF16, int VEC, int U> __device__ __forceinline__ void load_step(typename Chunk<BF16, VEC>::raw (&raw)[U], const Walk<BF16, VEC> &from, int left)
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u < left) raw[u] = ONCE ? Chunk<BF16, VEC>::load_once(from.at(u)) : Chunk<BF16, VEC>::load(from.at(u));
+}
 // A chunk of an output that may be an input itself: the columns that the last chunk shares with its neighbour are the neighbour's, which may have replaced
 // them before this thread read them.
 template <bool BF16, int VEC> __device__ __forceinline__ void put_chunk(typename Chunk<BF16, 1>::element *to, const float (&v)[VEC], const Columns &c, const Seat &s)
@@ -625,11 +645,6 @@ template <bool BF16, int VEC> __device__ __forceinline__ void put_chunk(typename
             if (i >= own) Element<BF16>::put(to + i, v[i]);
     }
 }
-template <bool BF16> __device__ __forceinline__ auto *channel_of(const Rows &v, int64_t point, int channel)
-{
-    return static_cast<typename Chunk<BF16, 1>::element *>(v.p) + point * v.point_stride + channel;
-}
-
 // A thread's own mean and squared distances first, step by step, then the workgroup's about its mean: sum of (M2 + n (mean - all)^2).
 template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_part_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
 {
@@ -643,25 +658,25 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     const int cg_tile = t.slices == 1 ? cg : c.width;    // a slice is all that a tile has of its group
     GroupSum<VEC, UNIT> sums = {lds, t, c, cg_tile};
     float *mean_of = lds + t.threads * NV, *m2_of = mean_of + c.groups;
-    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
-    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at);
+    const Stretch stretch = stretch_of(t, piece, s.ty, a.shape.positions);
+    Walk<BF16, VEC> x(a.x, n, stretch.first, c.first + s.at, t.down);
     float mean[NV], m2[NV], have = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) mean[i] = m2[i] = 0.f;
-    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+    for (int left = stretch.left; left > 0; left -= U, x.advance(U)) {
         typename C::raw raw[U];
-        walk.template load<false>(raw, x, a.x.position_stride, p);
+        load_step<false>(raw, x, left);
         auto step = [&](auto all) {
-            const int rows = all() ? U : static_cast<int>((walk.end - p + t.down - 1) / t.down);
-            float v[U][VEC], sum[NV], brought[NV];
+            const int rows = all() ? U : left;
+            float v[U][VEC], sum[NV];
 #pragma unroll
             for (int i = 0; i < NV; ++i) sum[i] = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (!all() && u >= rows) break;
                 C::widen(raw[u], v[u]);
-                gather<VEC, UNIT>(brought, v[u]);
 #pragma unroll
-                for (int i = 0; i < NV; ++i) sum[i] += all() || u < rows ? brought[i] : 0.f;
+                for (int i = 0; i < VEC; ++i) sum[i / UNIT] += v[u][i];
             }
             const float fresh = static_cast<float>(rows * UNIT), share = 1.f / fresh, total = have + fresh;
             const float part = fresh / total;
@@ -684,15 +699,15 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
             }
             have = total;
         };
-        if (p + (U - 1) * t.down < walk.end) step(std::true_type());
+        if (left >= U) step(std::true_type());
         else step(std::false_type());
     }
     float brought[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) brought[i] = have * mean[i];
     sums(s, brought, mean_of);
-    const int64_t begin = int64_t(piece) * t.down * t.k;
-    const float count = static_cast<float>(walk.end - begin) * (c.width / c.groups);
+    const int rows = min(t.down * t.k, a.shape.positions - piece * t.down * t.k);
+    const float count = static_cast<float>(rows) * (c.width / c.groups);
     for (int g = threadIdx.x; g < c.groups; g += blockDim.x) mean_of[g] /= count;
     __syncthreads();
     float all[VEC];
@@ -703,7 +718,7 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     for (int g = threadIdx.x; g < c.groups; g += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + g] = f2{mean_of[g], m2_of[g]};
 }
 
-template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_join_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
+template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds__(256) norm_join_forward_kernel(NormArgs a, Tiling t, Parts parts, int64_t first_point)
 {
     constexpr int U = 4;
     using C = Chunk<BF16, VEC>;
@@ -714,11 +729,10 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     float *mean = lds, *rstd = mean + c.groups;
-    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
-    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at);
-    auto *y = channel_of<BF16>(a.y, n, c.first + s.at);
+    const Stretch stretch = stretch_of(t, piece, s.ty, a.shape.positions);
+    Walk<BF16, VEC> x(a.x, n, stretch.first, c.first + s.at, t.down), y(a.y, n, stretch.first, c.first + s.at, t.down);
     typename C::raw raw[U];
-    walk.template load<true>(raw, x, a.x.position_stride, walk.first);                   // on its way while the statistics are joined
+    load_step<true>(raw, x, stretch.left);               // on its way while the statistics are joined
     join_parts(parts, t, c, n, tile, [&](int g, int lane, int lanes, int first_tile) {
         // the values of piece i of slice j: rows times columns
         auto values = [&](int i, int j) {
@@ -749,31 +763,27 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     });
     __syncthreads();
     if (!s.has) return;
-    float m[VEC], r[VEC], gamma[VEC], beta[VEC];
+    float m[VEC], r[VEC];
     const int cg_tile = t.slices == 1 ? cg : c.width;
     spread<VEC, UNIT>(m, mean, s, c, cg_tile);
     spread<VEC, UNIT>(r, rstd, s, c, cg_tile);
-    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
-    read_floats(beta, a.beta, c.first + s.at, 0.f);
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) gamma[v] *= r[v];
-    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
-        if (p != walk.first) walk.template load<true>(raw, x, a.x.position_stride, p);
+    const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+    for (int left = stretch.left; left > 0; left -= U) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = p + u * t.down;
-            if (at >= walk.end) break;
+            if (u >= left) break;
             float v[VEC];
             C::widen(raw[u], v);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = fmaf(v[i] - m[i], gamma[i], beta[i]);
-            activate(a.activation, v);
-            put_chunk<BF16, VEC>(y + at * a.y.position_stride, v, c, s);
+            finish(v);
+            put_chunk<BF16, VEC>(y.at(u), v, c, s);
         }
+        x.advance(U);
+        y.advance(U);
+        load_step<true>(raw, x, left - U);
     }
 }
 
-template <bool BF16, int VEC, int UNIT>
+template <bool BF16, int VEC, int UNIT, int ACT>
 __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point, float *parts_gamma, float *parts_beta)
 {
     constexpr int U = 4, NV = VEC / UNIT;
@@ -787,30 +797,26 @@ __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a,
     GroupSum<VEC, UNIT> sums = {lds, t, c, cg_tile};
     const int room = t.threads * NV;
     float *A_of = lds + 2 * room, *B_of = A_of + c.groups;
-    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
-    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at), *dy = channel_of<BF16>(a.dy, n, c.first + s.at);
-    float m[VEC], r[VEC], s1[VEC], s2[VEC], gamma[VEC], beta[VEC];
-    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
-    read_floats(beta, a.beta, c.first + s.at, 0.f);
-    read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
+    const Stretch stretch = stretch_of(t, piece, s.ty, a.shape.positions);
+    Walk<BF16, VEC> x(a.x, n, stretch.first, c.first + s.at, t.down), dy(a.dy, n, stretch.first, c.first + s.at, t.down);
+    Gradient<BF16, VEC, ACT> g;
+    float s1[VEC], s2[VEC];
+    read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
+    read_floats(g.beta, a.beta, c.first + s.at, 0.f);
+    read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, n, cg);
 #pragma unroll
     for (int v = 0; v < VEC; ++v) s1[v] = s2[v] = 0.f;
-    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
+    for (int left = stretch.left; left > 0; left -= U, x.advance(U), dy.advance(U)) {
         typename C::raw raw[U], raw_d[U];
-        walk.template load<false>(raw, x, a.x.position_stride, p);
-        walk.template load<false>(raw_d, dy, a.dy.position_stride, p);
+        load_step<false>(raw, x, left);
+        load_step<false>(raw_d, dy, left);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (p + u * t.down >= walk.end) break;
-            float h[VEC], z[VEC], d[VEC];
+            if (u >= left) break;
+            float h[VEC], d[VEC];
             C::widen(raw[u], h);
             C::widen(raw_d[u], d);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                h[v] = (h[v] - m[v]) * r[v];
-                z[v] = fmaf(h[v], gamma[v], beta[v]);
-            }
-            through_slope(a.activation, z, d);
+            g.slopes(h, d);
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 s1[v] += d[v];
@@ -823,24 +829,11 @@ __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a,
         add_columns(s2, s.has, s.at, s.ty, t.down, c.width, lds, give(parts_gamma));
         add_columns(s1, s.has, s.at, s.ty, t.down, c.width, lds, give(parts_beta));
     }
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-        s1[v] *= gamma[v];
-        s2[v] *= gamma[v];
-    }
-    float brought[NV];
-    gather<VEC, UNIT>(brought, s1);
-    sums.put(s, brought, lds);
-    gather<VEC, UNIT>(brought, s2);
-    sums.put(s, brought, lds + room);
-    __syncthreads();
-    sums.add(lds, A_of);
-    sums.add(lds + room, B_of);
-    __syncthreads();
-    for (int g = threadIdx.x; g < c.groups; g += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + g] = f2{A_of[g], B_of[g]};
+    bring<VEC, UNIT>(sums, s, g.gamma, s1, s2, room, A_of, B_of);
+    for (int q = threadIdx.x; q < c.groups; q += blockDim.x) parts.pair[parts.at(t, local, tile, piece) + q] = f2{A_of[q], B_of[q]};
 }
 
-template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) norm_join_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point)
+template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds__(256) norm_join_backward_kernel(NormGradArgs a, Tiling t, Parts parts, int64_t first_point)
 {
     constexpr int U = 4;
     using C = Chunk<BF16, VEC>;
@@ -851,12 +844,11 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     const Columns c = columns_of(a.shape, a.groups, t, tile);
     const Seat s = take_seat<VEC>(t, c);
     float *A_of = lds, *B_of = A_of + c.groups;
-    const PieceWalk<BF16, VEC, U> walk(t, piece, s.ty, a.shape.positions);
-    const auto *x = channel_of<BF16>(a.x, n, c.first + s.at), *dy = channel_of<BF16>(a.dy, n, c.first + s.at);
-    auto *dx = channel_of<BF16>(a.dx, n, c.first + s.at);
+    const Stretch stretch = stretch_of(t, piece, s.ty, a.shape.positions);
+    Walk<BF16, VEC> x(a.x, n, stretch.first, c.first + s.at, t.down), dy(a.dy, n, stretch.first, c.first + s.at, t.down), dx(a.dx, n, stretch.first, c.first + s.at, t.down);
     typename C::raw raw[U], raw_d[U];
-    walk.template load<true>(raw, x, a.x.position_stride, walk.first);
-    walk.template load<true>(raw_d, dy, a.dy.position_stride, walk.first);
+    load_step<true>(raw, x, stretch.left);
+    load_step<true>(raw_d, dy, stretch.left);
     const double all = static_cast<double>(a.shape.positions) * cg;
     join_parts(parts, t, c, n, tile, [&](int g, int lane, int lanes, int first_tile) {
         double sum_A = 0.0, sum_B = 0.0;
@@ -874,37 +866,34 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
             B_of[g] = static_cast<float>(sum_B / all);
         }
     });
-    float m[VEC], r[VEC], gamma[VEC], beta[VEC], A[VEC], B[VEC];
-    read_floats(gamma, a.gamma, c.first + s.at, 1.f);
-    read_floats(beta, a.beta, c.first + s.at, 0.f);
-    read_stats<VEC, UNIT>(m, r, a, s, c, n, cg);
+    Gradient<BF16, VEC, ACT> g;
+    float A[VEC], B[VEC];
+    read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
+    read_floats(g.beta, a.beta, c.first + s.at, 0.f);
+    read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, n, cg);
     __syncthreads();
     if (!s.has) return;
     const int cg_tile = t.slices == 1 ? cg : c.width;
     spread<VEC, UNIT>(A, A_of, s, c, cg_tile);
     spread<VEC, UNIT>(B, B_of, s, c, cg_tile);
-    for (int64_t p = walk.first; p < walk.end; p += U * t.down) {
-        if (p != walk.first) {
-            walk.template load<true>(raw, x, a.x.position_stride, p);
-            walk.template load<true>(raw_d, dy, a.dy.position_stride, p);
-        }
+    const Correction<VEC> dx_of(A, B, 1.f);
+    for (int left = stretch.left; left > 0; left -= U) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t at = p + u * t.down;
-            if (at >= walk.end) break;
-            float h[VEC], z[VEC], d[VEC];
+            if (u >= left) break;
+            float h[VEC], d[VEC];
             C::widen(raw[u], h);
             C::widen(raw_d[u], d);
+            g.slopes(h, d);
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) {
-                h[v] = (h[v] - m[v]) * r[v];
-                z[v] = fmaf(h[v], gamma[v], beta[v]);
-            }
-            through_slope(a.activation, z, d);
-#pragma unroll
-            for (int v = 0; v < VEC; ++v) d[v] = r[v] * (fmaf(gamma[v], d[v], -A[v]) - h[v] * B[v]);
-            put_chunk<BF16, VEC>(dx + at * a.dx.position_stride, d, c, s);
+            for (int v = 0; v < VEC; ++v) d[v] = dx_of(g, h[v], d[v], v);
+            put_chunk<BF16, VEC>(dx.at(u), d, c, s);
         }
+        x.advance(U);
+        dy.advance(U);
+        dx.advance(U);
+        load_step<true>(raw, x, left - U);
+        load_step<true>(raw_d, dy, left - U);
     }
 }
 
@@ -989,10 +978,13 @@ Tiling cut(const LayerShape &s, int groups)
         while (across_for(s, groups, t.tiles) > t.threads) ++t.tiles;
         t.across = across_for(s, groups, t.tiles);
     }
-    // positions of a thread: few where that gives the chip enough workgroups, many where it has enough anyway
+    // Positions of a thread: many where the chip has enough workgroups anyway.  Forward, us, for 8 / 16 / 32 / 64: 64 x 4 096 x 512 bf16 237 / 177 / 176 / 172,
+    // 64 x 1 024 x 320 41 / 34 / 39 / 53, 16 x 16 384 x 64 27 / 28 / 32 / 50; backward 316 / 279 / 278 / 274, 64 / 57 / 64 / 79, 45 / 46 / 52 / 78.
     t.down = t.threads / t.across;
     t.k = 8;
-    while (t.k < 32 && s.points * t.tiles * (int64_t(s.positions) / (int64_t(t.down) * t.k)) > 16 * kUnits) t.k *= 2;
+    auto workgroups = [&](int k) { return s.points * t.tiles * (int64_t(s.positions) / (int64_t(t.down) * k)); };
+    if (workgroups(16) >= 2 * kUnits) t.k = 16;
+    while (t.k >= 16 && t.k < 64 && workgroups(2 * t.k) >= 4 * kUnits) t.k *= 2;
     t.pieces = ceil_div(s.positions, int64_t(t.down) * t.k);
     t.down = std::min(t.down, s.positions);
     fold_columns(&t);
@@ -1000,13 +992,9 @@ Tiling cut(const LayerShape &s, int groups)
 }
 int most_groups(const Tiling &t, int groups) { return t.slices > 1 ? 1 : ceil_div(groups, t.tiles); }
 
-// points of a pair of launches: what they read twice stays in the last-level cache
-int64_t batch_points(const LayerShape &s, const Tiling &t, int tensors)
-{
-    const int64_t bytes = int64_t(s.positions) * s.channels * (s.bf16 ? 2 : 4) * tensors;
-    const int64_t fit = (int64_t(96) << 20) / bytes;
-    return std::max<int64_t>(1, std::min({s.points, std::max<int64_t>(fit, 1), (int64_t(1) << 22) / t.pieces}));
-}
+// Points of a pair of launches: as many as a grid takes.  (Fewer, so that what is read twice comes from the last-level cache, cost more at the launches' ends
+// than they gain: 64 x 4 096 x 512 bf16, points of 96 MB at a time / of 192 / all: forward 213 / 196 / 176 us, backward 365 / 320 / 279.)
+int64_t batch_points(const LayerShape &s, const Tiling &t) { return std::max<int64_t>(1, std::min<int64_t>(s.points, (int64_t(1) << 22) / t.pieces)); }
 
 template <typename F> void with_k(int k, F f)
 {
@@ -1022,17 +1010,24 @@ template <typename F> void with_types(const LayerShape &s, int groups, F f)
 {
     using Yes = std::true_type;
     using No = std::false_type;
-    const int vec = vec_of(s), cg = s.channels / groups, unit = cg % vec == 0 ? vec : vec % cg == 0 ? cg : 1;
-    auto with = [&](auto bf16, auto v) {
-        constexpr int V = v();
-        if (unit == V) f(bf16, v, std::integral_constant<int, V>());
-        else if (V > 4 && unit == 4) f(bf16, v, std::integral_constant<int, V >= 4 ? 4 : 1>());
-        else if (V > 2 && unit == 2) f(bf16, v, std::integral_constant<int, V >= 2 ? 2 : 1>());
+    const int vec = vec_of(s), cg = s.channels / groups;
+    auto with = [&](auto bf16, auto v) {                 // a load's, half a load's, one
+        constexpr int V = v(), HALF = V > 1 ? V / 2 : 1;
+        if (cg % V == 0) f(bf16, v, v);
+        else if (cg == HALF) f(bf16, v, std::integral_constant<int, HALF>());
         else f(bf16, v, std::integral_constant<int, 1>());
     };
     if (vec == 1) s.bf16 ? with(Yes(), std::integral_constant<int, 1>()) : with(No(), std::integral_constant<int, 1>());
     else if (s.bf16) with(Yes(), std::integral_constant<int, 8>());
     else with(No(), std::integral_constant<int, 4>());
+}
+template <typename F> void with_activation(int kind, F f)
+{
+    switch (kind) {
+    case 0: f(std::integral_constant<int, 0>()); break;
+    case 1: f(std::integral_constant<int, 1>()); break;
+    default: f(std::integral_constant<int, 2>()); break;
+    }
 }
 template <typename F> void with_lanes(int lanes, F f)
 {
@@ -1103,7 +1098,7 @@ BackwardRoom room_of(const LayerShape &s, int groups, const BackwardPlan &p, con
     BackwardRoom r;
     r.table = align_up(static_cast<size_t>(rows) * s.channels * sizeof(float));
     r.beside = align_up(static_cast<size_t>(rows_beside(most, runs)) * s.channels * sizeof(float));
-    r.pairs = p.cut ? static_cast<size_t>(batch_points(s, p.t, 2)) * p.t.tiles * p.t.pieces * most_groups(p.t, groups) * sizeof(f2) : 0;
+    r.pairs = p.cut ? static_cast<size_t>(batch_points(s, p.t)) * p.t.tiles * p.t.pieces * most_groups(p.t, groups) * sizeof(f2) : 0;
     return r;
 }
 
@@ -1113,7 +1108,7 @@ size_t norm_forward_bytes(const LayerShape &s, int groups)
 {
     if (s.points == 0 || lanes_per_group(s, groups) || tile(s, groups, kForwardThreads, kForwardChunks).k) return 0;
     const Tiling t = cut(s, groups);
-    return static_cast<size_t>(batch_points(s, t, 1)) * t.tiles * t.pieces * most_groups(t, groups) * sizeof(f2);
+    return static_cast<size_t>(batch_points(s, t)) * t.tiles * t.pieces * most_groups(t, groups) * sizeof(f2);
 }
 
 size_t norm_backward_bytes(const LayerShape &s, int groups, const int64_t *bounds, int runs)
@@ -1130,7 +1125,9 @@ hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t s
         const int64_t length = rows_of_workgroup(s, across, 16, 1);
         const dim3 grid(ceil_div(s.channels / (s.bf16 ? 8 : 4), across), ceil_div(s.points, length));
         with_lanes(lanes, [&](auto l) {
-            (s.bf16 ? norm_rows_forward_kernel<true, l()> : norm_rows_forward_kernel<false, l()>)<<<grid, 256, 0, stream>>>(a, across, length);
+            with_activation(a.activation, [&](auto act) {
+                (s.bf16 ? norm_rows_forward_kernel<true, l(), act()> : norm_rows_forward_kernel<false, l(), act()>)<<<grid, 256, 0, stream>>>(a, across, length);
+            });
         });
         return hipGetLastError();
     }
@@ -1140,20 +1137,23 @@ hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t s
             with_k(t.k, [&](auto k) {
                 const dim3 grid(static_cast<unsigned>(std::min<int64_t>((s.points + t.side - 1) / t.side, 1 << 20)), t.tiles);
                 const size_t lds = (t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float);
-                (t.threads > 512 ? norm_tile_forward_kernel<bf16(), vec(), k(), unit(), 1024> : norm_tile_forward_kernel<bf16(), vec(), k(), unit(), 512>)<<<grid, t.threads, lds, stream>>>(a, t);
+                with_activation(a.activation, [&](auto act) {
+                    constexpr int B = bf16(), V = vec(), K = k(), U = unit(), A = act();
+                    (t.threads > 512 || K < 8 ? norm_tile_forward_kernel<B, V, K, U, A, 1024> : norm_tile_forward_kernel<B, V, K, U, A, K < 8 ? 1024 : 512>)<<<grid, t.threads, lds, stream>>>(a, t);
+                });
             });
         });
         return hipGetLastError();
     }
     const Tiling c = cut(s, a.groups);
     const Parts parts = {static_cast<f2 *>(workspace), most_groups(c, a.groups)};
-    const int64_t batch = batch_points(s, c, 1);
+    const int64_t batch = batch_points(s, c);
     for (int64_t n = 0; n < s.points; n += batch) {
         const dim3 grid(static_cast<unsigned>(std::min(batch, s.points - n) * c.pieces), c.tiles);
         with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
             const size_t tables = 2 * parts.stride * sizeof(float), lds = c.threads * (vec() / unit()) * sizeof(float) + tables;
             norm_part_forward_kernel<bf16(), vec(), unit()><<<grid, c.threads, lds, stream>>>(a, c, parts, n);
-            norm_join_forward_kernel<bf16(), vec(), unit()><<<grid, c.threads, tables, stream>>>(a, c, parts, n);
+            with_activation(a.activation, [&](auto act) { norm_join_forward_kernel<bf16(), vec(), unit(), act()><<<grid, c.threads, tables, stream>>>(a, c, parts, n); });
         });
     }
     return hipGetLastError();
@@ -1179,15 +1179,17 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
         if (p.cut) {
             const Tiling &t = p.t;
             const Parts parts = {reinterpret_cast<f2 *>(at + 2 * room.table + 2 * room.beside), most_groups(t, a.groups)};
-            const int64_t batch = batch_points(s, t, 2);
+            const int64_t batch = batch_points(s, t);
             for (int64_t n = 0; n < s.points; n += batch) {
                 const dim3 grid(static_cast<unsigned>(std::min(batch, s.points - n) * t.pieces), t.tiles);
                 with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
                     const size_t tables = 2 * parts.stride * sizeof(float), columns = t.threads * vec() * sizeof(float);
                     const size_t lds = std::max(2 * t.threads * (vec() / unit()) * sizeof(float) + tables, columns);
                     float *to_gamma = sums ? parts_gamma + n * t.pieces * s.channels : nullptr, *to_beta = sums ? parts_beta + n * t.pieces * s.channels : nullptr;
-                    norm_part_backward_kernel<bf16(), vec(), unit()><<<grid, t.threads, lds, stream>>>(a, t, parts, n, to_gamma, to_beta);
-                    if (a.dx.p) norm_join_backward_kernel<bf16(), vec(), unit()><<<grid, t.threads, tables, stream>>>(a, t, parts, n);
+                    with_activation(a.activation, [&](auto act) {
+                        norm_part_backward_kernel<bf16(), vec(), unit(), act()><<<grid, t.threads, lds, stream>>>(a, t, parts, n, to_gamma, to_beta);
+                        if (a.dx.p) norm_join_backward_kernel<bf16(), vec(), unit(), act()><<<grid, t.threads, tables, stream>>>(a, t, parts, n);
+                    });
                 });
             }
         }
@@ -1205,7 +1207,9 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
             const int across = across_of(s, p.lanes);
             const dim3 grid(ceil_div(s.channels / (s.bf16 ? 8 : 4), across), count);
             with_lanes(p.lanes, [&](auto l) {
-                (s.bf16 ? norm_rows_backward_kernel<true, l()> : norm_rows_backward_kernel<false, l()>)<<<grid, 256, 0, stream>>>(a, across, pieces, parts_gamma, parts_beta);
+                with_activation(a.activation, [&](auto act) {
+                    (s.bf16 ? norm_rows_backward_kernel<true, l(), act()> : norm_rows_backward_kernel<false, l(), act()>)<<<grid, 256, 0, stream>>>(a, across, pieces, parts_gamma, parts_beta);
+                });
             });
         } else if (count > 0) {
             const Tiling &t = p.t;
@@ -1214,7 +1218,9 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
                     constexpr int K = k() < kBackwardChunks ? k() : kBackwardChunks;
                     const size_t columns = t.threads * vec() * sizeof(float);
                     const size_t lds = std::max((2 * t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float), columns);
-                    norm_tile_backward_kernel<bf16(), vec(), K, unit()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                    with_activation(a.activation, [&](auto act) {
+                        norm_tile_backward_kernel<bf16(), vec(), K, unit(), act()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                    });
                 });
             });
         }

@@ -8,7 +8,9 @@
 
 namespace cr {
 
-typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef float f4u __attribute__((ext_vector_type(4), aligned(4)));       // the same in memory, on any boundary that the elements have
 typedef unsigned u4h __attribute__((ext_vector_type(4), aligned(2)));
 typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
 typedef float f2 __attribute__((ext_vector_type(2)));
@@ -47,21 +49,23 @@ template <> struct Chunk<true, 1> {
 };
 template <> struct Chunk<false, 4> {
     using element = float;
-    using raw = f4u;
-    static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const raw *>(p); }
-    static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const raw *>(p)); }
-    static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<raw *>(p) = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, reinterpret_cast<raw *>(p)); }
+    using raw = f4;
+    using memory = f4u;
+    static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
+    static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
+    static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(static_cast<memory>(r), reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
     static __device__ __forceinline__ raw narrow(const float (&v)[4]) { return raw{v[0], v[1], v[2], v[3]}; }
 };
 template <> struct Chunk<true, 8> {
     using element = uint16_t;
-    using raw = u4h;
-    static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const raw *>(p); }
-    static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const raw *>(p)); }
-    static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<raw *>(p) = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, reinterpret_cast<raw *>(p)); }
+    using raw = u4;
+    using memory = u4h;
+    static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
+    static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
+    static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(static_cast<memory>(r), reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[8])
     {
         v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
@@ -155,6 +159,9 @@ template <typename P> __device__ __forceinline__ P *scalar(P *p)
     asm("" : "+s"(at));
     return (P *)reinterpret_cast<__attribute__((address_space(1))) P *>(at);          // an address in global memory
 }
+// Says that a loaded value is needed from here on, so that its load is not moved behind a branch to where it is first used: several loads asked for together
+// stay together.
+template <typename R> __device__ __forceinline__ void hold(R &raw) { asm volatile("" : "+v"(raw)); }
 // A value at an address that is the same for all lanes, through the scalar cache: waiting for it is not waiting for vector loads.
 template <typename P> __device__ __forceinline__ P scalar_load(const P *p)
 {

@@ -6,6 +6,7 @@
 //
 //   norm_rows_*    points of one position, groups of 1 to 64 chunks, a power of two: a group is a few lanes, no workgroup meets
 //   norm_tile_*    a point's group (or some of them, or several points) in the registers of a workgroup, read once
+//   norm_deep_*    the same for several points of few positions at a time
 //   norm_part_*, norm_join_*   larger groups: pieces of a group leave their sums, then every piece is read again
 #include "runs_device.h"
 
@@ -198,6 +199,7 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
 struct Tiling {
     int tiles, slices, unit, across, down, side, threads, k;             // slices begin at multiples of `unit` channels of the group
     int pieces;                  // of a point's positions, down * k each
+    int deep;                    // points of a thread, or 0: it has one point's positions (k of them)
     int fold;                    // the seats of a column in a wavefront are `across` lanes apart, and the wavefront has one point's: they are added up before LDS
 };
 struct Columns {
@@ -265,15 +267,16 @@ template <int VEC, int UNIT> struct GroupSum {
             for (int i = 0; i < NV; ++i) to[(s.side * t.down + s.ty) * width + s.at / UNIT + i] = value[i];
         }
     }
-    __device__ __forceinline__ void add(const float *from, float *out)
+    // `deep` tables of values, so many floats apart; the sums follow each other as the tables do
+    __device__ __forceinline__ void add(const float *from, float *out, int deep = 1, int apart = 0)
     {
-        const int per = cg / UNIT, width = c.width / UNIT, sums = t.side * c.groups, rows = t.fold ? t.down * t.across / 64 : t.down;
+        const int per = cg / UNIT, width = c.width / UNIT, at_once = t.side * c.groups, sums = deep * at_once, rows = t.fold ? t.down * t.across / 64 : t.down;
         int lanes = 64;          // per sum: a power of two, so that the sums share out the workgroup's threads
         while (lanes > 1 && lanes * sums > static_cast<int>(blockDim.x)) lanes /= 2;
         const int lane = threadIdx.x % lanes, step_row = lanes / per, step_col = lanes % per;
         for (int q = threadIdx.x / lanes; q < sums; q += blockDim.x / lanes) {
-            const int side = q / c.groups, g = q % c.groups;
-            const float *base = from + side * rows * width + g * per;
+            const int level = q / at_once, side = q % at_once / c.groups, g = q % c.groups;
+            const float *base = from + level * apart + side * rows * width + g * per;
             int row = lane / per, col = lane % per;
             float sum = 0.f;
             while (row < rows) {
@@ -336,6 +339,8 @@ template <bool BF16, int VEC> struct Walk {
     {
     }
     __device__ __forceinline__ T *at(int k) const { return scalar(base + k * step) + offset; }
+    // for a load that nobody branches around, where a branch would make every wait one for all loads: what is not there is the first once more
+    __device__ __forceinline__ const T *at_or_first(int k, bool there) const { return base + (offset + (there ? k * step : 0)); }
     __device__ __forceinline__ void advance(int k) { base += k * step; }
 };
 // positions of a thread that exist: of K from `first` on, `down` apart
@@ -415,10 +420,11 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT, int MOST> __global__ voi
     for (int64_t n0 = int64_t(blockIdx.x) * t.side; n0 < a.shape.points; n0 += int64_t(gridDim.x) * t.side) {
         const int64_t n = n0 + s.side;
         typename C::raw raw[K];
-        const Walk<BF16, VEC> x(a.x, min(n, a.shape.points - 1), s.ty, c.first + s.at, t.down);
+        const Walk<BF16, VEC> x(a.x, min(n, a.shape.points - 1), min(s.ty, positions - 1), c.first + s.at, t.down);
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-            if (exists(s.ty, k, t.down, positions)) raw[k] = C::load_once(x.at(k));
+        for (int k = 0; k < K; ++k) raw[k] = C::load_once(x.at_or_first(k, exists(s.ty, k, t.down, positions)));
+#pragma unroll
+        for (int k = 0; k < K; ++k) hold(raw[k]);
         tile_moments<BF16, VEC, K, UNIT>(raw, s, positions, t, c, cg, count, sums, mean, rstd);
         for (int q = threadIdx.x; q < t.side * c.groups; q += blockDim.x) {
             rstd[q] = 1.f / sqrtf(rstd[q] / count + a.eps);
@@ -446,6 +452,84 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT, int MOST> __global__ voi
             }
         }
         __syncthreads();                                 // before the tables are another point's
+    }
+}
+
+// Points of few positions: a thread has one position (if that many) of K points, which share the barriers.
+template <bool BF16, int VEC, int K, int UNIT, int ACT> __global__ void __launch_bounds__(512) norm_deep_forward_kernel(NormArgs a, Tiling t)
+{
+    using C = Chunk<BF16, VEC>;
+    constexpr int NV = VEC / UNIT;
+    extern __shared__ float lds[];
+    const int cg = a.shape.channels / a.groups, tile = blockIdx.y, positions = a.shape.positions;
+    const Columns c = columns_of(a.shape, a.groups, t, tile);
+    const Seat s = take_seat<VEC>(t, c);
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
+    const int room = t.threads * NV, tables = t.side * c.groups;
+    float *mean = lds + K * room, *rstd = mean + K * tables;
+    const float count = static_cast<float>(positions) * cg, share = 1.f / count;
+    const bool there = s.ty < positions;
+    for (int64_t n0 = int64_t(blockIdx.x) * t.side * K; n0 < a.shape.points; n0 += int64_t(gridDim.x) * t.side * K) {
+        const int64_t n = n0 + s.side;                   // and n + side, ...
+        typename C::raw raw[K];
+        const Walk<BF16, VEC> x(a.x, 0, min(s.ty, positions - 1), c.first + s.at, t.down);
+#pragma unroll
+        for (int k = 0; k < K; ++k) raw[k] = C::load_once(x.base + (x.offset + min(n + k * t.side, a.shape.points - 1) * a.x.point_stride));
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            hold(raw[k]);
+            float v[VEC], brought[NV];
+            C::widen(raw[k], v);
+            gather<VEC, UNIT>(brought, v);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) brought[i] = there ? brought[i] : 0.f;
+            sums.put(s, brought, lds + k * room);
+        }
+        __syncthreads();
+        sums.add(lds, mean, K, room);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float v[VEC], m[VEC], brought[NV];
+            C::widen(raw[k], v);
+            spread<VEC, UNIT>(m, mean + k * tables, s, c, cg);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                v[i] = fmaf(-m[i], share, v[i]);
+                v[i] *= v[i];
+            }
+            gather<VEC, UNIT>(brought, v);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) brought[i] = there ? brought[i] : 0.f;
+            sums.put(s, brought, lds + k * room);
+        }
+        __syncthreads();
+        sums.add(lds, rstd, K, room);
+        __syncthreads();
+        for (int q = threadIdx.x; q < K * tables; q += blockDim.x) {
+            mean[q] *= share;
+            rstd[q] = 1.f / sqrtf(fmaf(rstd[q], share, a.eps));
+            const int64_t point = n0 + q / c.groups;     // tables of points n0, n0 + 1, ...
+            if (a.mean && point < a.shape.points) {
+                a.mean[point * a.groups + c.group + q % c.groups] = mean[q];
+                a.rstd[point * a.groups + c.group + q % c.groups] = rstd[q];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (s.has && there && n + k * t.side < a.shape.points) {
+                float v[VEC], m[VEC], r[VEC];
+                spread<VEC, UNIT>(m, mean + k * tables, s, c, cg);
+                spread<VEC, UNIT>(r, rstd + k * tables, s, c, cg);
+                const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+                C::widen(raw[k], v);
+                finish(v);
+                const Walk<BF16, VEC> y(a.y, n + k * t.side, s.ty, c.first + s.at, t.down);
+                C::store(y.base + y.offset, C::narrow(v));
+            }
+        }
+        __syncthreads();                                 // before the tables are other points'
     }
 }
 
@@ -514,7 +598,7 @@ __device__ __forceinline__ void bring(GroupSum<VEC, UNIT> &sums, const Seat &s, 
 }
 // A workgroup goes through the points of a piece of a run, `side` at a time.
 template <bool BF16, int VEC, int K, int UNIT, int ACT>
-__global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a, Tiling t, Pieces pieces, float *parts_gamma, float *parts_beta)
+__global__ void __launch_bounds__(256) norm_tile_backward_kernel(NormGradArgs a, Tiling t, Pieces pieces, float *parts_gamma, float *parts_beta)
 {
     using C = Chunk<BF16, VEC>;
     extern __shared__ float lds[];
@@ -536,15 +620,19 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
         const int64_t n = min(n0 + s.side, piece.end - 1);
         const bool live = s.has && n0 + s.side < piece.end;
         typename C::raw raw[K], raw_d[K];
-        const Walk<BF16, VEC> x(a.x, n, s.ty, c.first + s.at, t.down), dy(a.dy, n, s.ty, c.first + s.at, t.down);
+        const int first = min(s.ty, positions - 1);
+        const Walk<BF16, VEC> x(a.x, n, first, c.first + s.at, t.down), dy(a.dy, n, first, c.first + s.at, t.down);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            if (exists(s.ty, k, t.down, positions)) {
-                raw[k] = C::load_once(x.at(k));
-                raw_d[k] = C::load_once(dy.at(k));
-            }
+            raw[k] = C::load_once(x.at_or_first(k, exists(s.ty, k, t.down, positions)));
+            raw_d[k] = C::load_once(dy.at_or_first(k, exists(s.ty, k, t.down, positions)));
         }
         read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, n, cg);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            hold(raw[k]);
+            hold(raw_d[k]);
+        }
         float dz[K][VEC], s1[VEC], s2[VEC];
 #pragma unroll
         for (int v = 0; v < VEC; ++v) s1[v] = s2[v] = 0.f;
@@ -598,6 +686,96 @@ __global__ void __launch_bounds__(512) norm_tile_backward_kernel(NormGradArgs a,
     add_columns(sum_beta, s.has, s.at, row, rows, c.width, lds, give(parts_beta));
 }
 
+template <bool BF16, int VEC, int K, int UNIT, int ACT>
+__global__ void __launch_bounds__(256) norm_deep_backward_kernel(NormGradArgs a, Tiling t, Pieces pieces, float *parts_gamma, float *parts_beta)
+{
+    using C = Chunk<BF16, VEC>;
+    constexpr int NV = VEC / UNIT;
+    extern __shared__ float lds[];
+    const int cg = a.shape.channels / a.groups, positions = a.shape.positions;
+    const Columns c = columns_of(a.shape, a.groups, t, blockIdx.y);
+    const Seat s = take_seat<VEC>(t, c);
+    GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
+    const int room = t.threads * NV, tables = t.side * c.groups;
+    float *A_of = lds + 2 * K * room, *B_of = A_of + K * tables;
+    const float share = 1.f / (static_cast<float>(positions) * cg);
+    const bool there = s.ty < positions;
+    Gradient<BF16, VEC, ACT> g;
+    float sum_gamma[VEC], sum_beta[VEC];
+    read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
+    read_floats(g.beta, a.beta, c.first + s.at, 0.f);
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) sum_gamma[v] = sum_beta[v] = 0.f;
+    const Piece piece = find_piece(pieces, blockIdx.x);
+    const Walk<BF16, VEC> x(a.x, 0, min(s.ty, positions - 1), c.first + s.at, t.down), dy(a.dy, 0, min(s.ty, positions - 1), c.first + s.at, t.down);
+    for (int64_t n0 = piece.begin; n0 < piece.end; n0 += t.side * K) {
+        typename C::raw raw[K], raw_d[K];
+        auto point = [&](int k) { return min(n0 + s.side + k * t.side, piece.end - 1); };
+        auto live = [&](int k) { return s.has && there && n0 + s.side + k * t.side < piece.end; };
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            raw[k] = C::load_once(x.base + (x.offset + point(k) * a.x.point_stride));
+            raw_d[k] = C::load_once(dy.base + (dy.offset + point(k) * a.dy.point_stride));
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            hold(raw[k]);
+            hold(raw_d[k]);
+        }
+        float dz[K][VEC];
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            float h[VEC], s1[VEC], s2[VEC], brought[NV];
+            C::widen(raw[k], h);
+            C::widen(raw_d[k], dz[k]);
+            read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, point(k), cg);
+            g.slopes(h, dz[k]);
+            const bool counts = live(k);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) {
+                s1[v] = counts ? dz[k][v] : 0.f;
+                s2[v] = s1[v] * h[v];
+                sum_beta[v] += s1[v];
+                sum_gamma[v] = fmaf(s1[v], h[v], sum_gamma[v]);
+                s1[v] *= g.gamma[v];
+                s2[v] *= g.gamma[v];
+            }
+            if (!a.dx.p) continue;
+            gather<VEC, UNIT>(brought, s1);
+            sums.put(s, brought, lds + k * room);
+            gather<VEC, UNIT>(brought, s2);
+            sums.put(s, brought, lds + (K + k) * room);
+        }
+        if (!a.dx.p) continue;
+        __syncthreads();
+        sums.add(lds, A_of, K, room);
+        sums.add(lds + K * room, B_of, K, room);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (live(k)) {
+                float h[VEC], A[VEC], B[VEC];
+                C::widen(raw[k], h);
+                spread<VEC, UNIT>(A, A_of + k * tables, s, c, cg);
+                spread<VEC, UNIT>(B, B_of + k * tables, s, c, cg);
+                read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, point(k), cg);
+                const Correction<VEC> dx_of(A, B, share);
+#pragma unroll
+                for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, g.h(h[v], v), dz[k][v], v);
+                const Walk<BF16, VEC> dx(a.dx, point(k), s.ty, c.first + s.at, t.down);
+                C::store(dx.base + dx.offset, C::narrow(h));
+            }
+        }
+        // the next step's sums are put where this one's were read before the last barrier, and its results written after another one
+    }
+    if (!parts_gamma) return;
+    __syncthreads();
+    auto give = [&](float *parts) { return [=](int col, float total) { parts[int64_t(blockIdx.x) * a.shape.channels + c.first + col] = total; }; };
+    const int row = s.side * t.down + s.ty, rows = t.side * t.down;
+    add_columns(sum_gamma, s.has, s.at, row, rows, c.width, lds, give(parts_gamma));
+    add_columns(sum_beta, s.has, s.at, row, rows, c.width, lds, give(parts_beta));
+}
+
 // ---- pieces of a point's groups ------------------------------------------------------------------------------------------------------------
 // parts[((point * tiles + tile) * pieces + piece) * (most groups of a tile) + group] = a pair of sums; forward: mean and M2, backward: A and B before
 // they are divided.
@@ -624,13 +802,21 @@ struct Stretch {
 __device__ __forceinline__ Stretch stretch_of(const Tiling &t, int piece, int ty, int positions)
 {
     const int64_t begin = int64_t(piece) * t.down * t.k, end = min(begin + int64_t(t.down) * t.k, int64_t(positions));
-    return {begin + ty, static_cast<int>((end - begin - ty + t.down - 1) / t.down)};     // none, or fewer, where ty is past the end
+    const int rows = static_cast<int>(end - begin);
+    return {begin + min(ty, rows - 1), (rows - ty + t.down - 1) / t.down};               // none where ty is past the end
 }
 template <bool ONCE, bool BF16, int VEC, int U> __device__ __forceinline__ void load_step(typename Chunk<BF16, VEC>::raw (&raw)[U], const Walk<BF16, VEC> &from, int left)
 {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u < left) raw[u] = ONCE ? Chunk<BF16, VEC>::load_once(from.at(u)) : Chunk<BF16, VEC>::load(from.at(u));
+    for (int u = 0; u < U; ++u) {
+        const auto *p = from.at_or_first(u, u < left);
+        raw[u] = ONCE ? Chunk<BF16, VEC>::load_once(p) : Chunk<BF16, VEC>::load(p);
+    }
+}
+template <int U, typename R> __device__ __forceinline__ void hold_step(R (&raw)[U])
+{
+#pragma unroll
+    for (int u = 0; u < U; ++u) hold(raw[u]);
 }
 // A chunk of an output that may be an input itself: the columns that the last chunk shares with its neighbour are the neighbour's, which may have replaced
 // them before this thread read them.
@@ -666,6 +852,7 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
     for (int left = stretch.left; left > 0; left -= U, x.advance(U)) {
         typename C::raw raw[U];
         load_step<false>(raw, x, left);
+        hold_step(raw);
         auto step = [&](auto all) {
             const int rows = all() ? U : left;
             float v[U][VEC], sum[NV];
@@ -769,6 +956,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
     spread<VEC, UNIT>(r, rstd, s, c, cg_tile);
     const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
     for (int left = stretch.left; left > 0; left -= U) {
+        hold_step(raw);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u >= left) break;
@@ -777,6 +965,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
             finish(v);
             put_chunk<BF16, VEC>(y.at(u), v, c, s);
         }
+        if (left <= U) break;
         x.advance(U);
         y.advance(U);
         load_step<true>(raw, x, left - U);
@@ -810,6 +999,8 @@ __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a,
         typename C::raw raw[U], raw_d[U];
         load_step<false>(raw, x, left);
         load_step<false>(raw_d, dy, left);
+        hold_step(raw);
+        hold_step(raw_d);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u >= left) break;
@@ -878,6 +1069,8 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
     spread<VEC, UNIT>(B, B_of, s, c, cg_tile);
     const Correction<VEC> dx_of(A, B, 1.f);
     for (int left = stretch.left; left > 0; left -= U) {
+        hold_step(raw);
+        hold_step(raw_d);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (u >= left) break;
@@ -889,6 +1082,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
             for (int v = 0; v < VEC; ++v) d[v] = dx_of(g, h[v], d[v], v);
             put_chunk<BF16, VEC>(dx.at(u), d, c, s);
         }
+        if (left <= U) break;
         x.advance(U);
         dy.advance(U);
         dx.advance(U);
@@ -915,7 +1109,7 @@ int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 constexpr int kMostGroups = 4096;                        // sums of a workgroup: with what they are made from they fit 64 KB of LDS
 constexpr int kPartThreads = 256;                        // of norm_part_* and norm_join_*
-constexpr int kForwardChunks = 8, kForwardThreads = 1024, kBackwardChunks = 4, kBackwardThreads = 512;   // of norm_tile_*
+constexpr int kForwardThreads = 1024, kBackwardThreads = 256;           // of norm_tile_*, at most; chunks of a thread: 8
 
 int vec_of(const LayerShape &s) { return s.channels < (s.bf16 ? 8 : 4) ? 1 : s.bf16 ? 8 : 4; }
 int across_for(const LayerShape &s, int groups, int tiles) { return ceil_div(int64_t(ceil_div(groups, tiles)) * (s.channels / groups), vec_of(s)); }
@@ -933,8 +1127,9 @@ void fold_columns(Tiling *t)
 // Tiles in registers: at most so many threads and chunks of each; k == 0: the point is too large, and is cut into pieces.  Small workgroups, of which
 // several share a compute unit and one loads while others add up; so tiles get narrower (down to a cache line of columns) before they get more threads,
 // and more threads rather than more chunks each where there are few of them.
-Tiling tile(const LayerShape &s, int groups, int most_threads, int most_chunks)
+Tiling tile(const LayerShape &s, int groups, bool backward)
 {
+    const int most_threads = backward ? kBackwardThreads : kForwardThreads, most_chunks = 8, vec = vec_of(s);
     const int cg = s.channels / groups, line = std::max(1, 128 / (cg * (s.bf16 ? 2 : 4)));
     Tiling t = {};
     t.slices = t.unit = t.side = t.pieces = 1;
@@ -958,6 +1153,14 @@ Tiling tile(const LayerShape &s, int groups, int most_threads, int most_chunks)
         t.side = std::max(1, std::min(t.threads / (t.across * t.down), kMostGroups / ceil_div(groups, tiles)));
         t.side = static_cast<int>(std::min<int64_t>(t.side, std::max<int64_t>(1, s.points)));
         fold_columns(&t);
+        // one position each: several points each, so long as there are enough for all workgroups and LDS for their sums
+        if (t.k == 1 && t.threads <= 512) {
+            const int values = cg % vec == 0 ? 1 : cg == vec / 2 ? 2 : vec;
+            auto room = [&](int deep) { return (size_t(deep) * t.threads * values + size_t(2) * deep * t.side * ceil_div(groups, tiles)) * (backward ? 2 : 1) * sizeof(float); };
+            // (the gradient of four, with a sum per channel, is more than the registers hold)
+            for (int deep = backward && values > 1 ? 2 : 4; deep > 1 && !t.deep; deep /= 2)
+                if (room(deep) <= size_t(48) << 10 && s.points * tiles >= int64_t(4) * kUnits * t.side * deep) t.deep = deep;
+        }
         return t;
     }
     return t;
@@ -1055,7 +1258,8 @@ int64_t points_of_piece(const LayerShape &s, const Tiling &t)
 {
     const int64_t wanted = std::max<int64_t>(1, kUnits * 8 / t.tiles);
     int64_t length = std::max<int64_t>((s.points + wanted - 1) / wanted, std::min<int64_t>(32 / std::min(s.positions, 32), (s.points + kUnits - 1) / kUnits));
-    return std::max<int64_t>((length + t.side - 1) / t.side * t.side, 1);
+    const int at_once = t.side * std::max(t.deep, 1);
+    return std::max<int64_t>((length + at_once - 1) / at_once * at_once, 1);
 }
 
 struct BackwardPlan {
@@ -1073,7 +1277,7 @@ BackwardPlan plan_backward(const LayerShape &s, int groups)
         p.length = rows_of_workgroup(s, across_of(s, p.lanes), 4, 4);
         return p;
     }
-    p.t = tile(s, groups, kBackwardThreads, kBackwardChunks);
+    p.t = tile(s, groups, true);
     if (p.t.k) {
         p.length = points_of_piece(s, p.t);
         return p;
@@ -1106,7 +1310,7 @@ BackwardRoom room_of(const LayerShape &s, int groups, const BackwardPlan &p, con
 
 size_t norm_forward_bytes(const LayerShape &s, int groups)
 {
-    if (s.points == 0 || lanes_per_group(s, groups) || tile(s, groups, kForwardThreads, kForwardChunks).k) return 0;
+    if (s.points == 0 || lanes_per_group(s, groups) || tile(s, groups, false).k) return 0;
     const Tiling t = cut(s, groups);
     return static_cast<size_t>(batch_points(s, t)) * t.tiles * t.pieces * most_groups(t, groups) * sizeof(f2);
 }
@@ -1131,7 +1335,19 @@ hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t s
         });
         return hipGetLastError();
     }
-    const Tiling t = tile(s, a.groups, kForwardThreads, kForwardChunks);
+    const Tiling t = tile(s, a.groups, false);
+    if (t.deep) {
+        with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
+            const int64_t at_once = t.side * t.deep;
+            const dim3 grid(static_cast<unsigned>(std::min<int64_t>((s.points + at_once - 1) / at_once, 1 << 20)), t.tiles);
+            const size_t lds = t.deep * (t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float);
+            with_activation(a.activation, [&](auto act) {
+                constexpr int B = bf16(), V = vec(), U = unit(), A = act();
+                (t.deep == 4 ? norm_deep_forward_kernel<B, V, 4, U, A> : norm_deep_forward_kernel<B, V, 2, U, A>)<<<grid, t.threads, lds, stream>>>(a, t);
+            });
+        });
+        return hipGetLastError();
+    }
     if (t.k) {
         with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
             with_k(t.k, [&](auto k) {
@@ -1213,13 +1429,22 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
             });
         } else if (count > 0) {
             const Tiling &t = p.t;
-            with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
+            if (t.deep) {
+                with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
+                    const size_t columns = t.threads * vec() * sizeof(float);
+                    const size_t lds = std::max(2 * t.deep * (t.threads * (vec() / unit()) + t.side * most_groups(t, a.groups)) * sizeof(float), columns);
+                    with_activation(a.activation, [&](auto act) {
+                        constexpr int B = bf16(), V = vec(), U = unit(), A = act();
+                        (t.deep == 4 ? norm_deep_backward_kernel<B, V, U == V ? 4 : 2, U, A> : norm_deep_backward_kernel<B, V, 2, U, A>)
+                            <<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                    });
+                });
+            } else with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
                 with_k(t.k, [&](auto k) {
-                    constexpr int K = k() < kBackwardChunks ? k() : kBackwardChunks;
                     const size_t columns = t.threads * vec() * sizeof(float);
                     const size_t lds = std::max((2 * t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float), columns);
                     with_activation(a.activation, [&](auto act) {
-                        norm_tile_backward_kernel<bf16(), vec(), K, unit(), act()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                        norm_tile_backward_kernel<bf16(), vec(), k(), unit(), act()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
                     });
                 });
             });

@@ -4,6 +4,7 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -11,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcodedreduce.so")
 SOURCES = ["gc_design.cpp", "tree_plan.cpp", "latency_model.cpp", "codedreduce.cpp", "kernels.hip"]
 LAYERS_LIB = os.path.join(HERE, "libcodedreduce_layers.so")
-LAYERS_SOURCES = ["layers.cpp", "norm_kernels.hip", "dropout_kernels.hip", "loss_kernels.hip"]
+LAYERS_SOURCES = ["layers.cpp", "norm_rows.hip", "norm_forward.hip", "norm_backward.hip", "dropout_kernels.hip", "loss_kernels.hip"]
 # the packed-fp32 target feature is switched off for all device code
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
@@ -25,8 +26,8 @@ def _library(lib: str, sources, verbose: bool) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     bdir = os.path.join(HERE, "_build")
     os.makedirs(bdir, exist_ok=True)
-    objs = []
-    for src in sources:
+
+    def compile_one(src):
         obj = os.path.join(bdir, src + ".o")
         cmd = [hipcc, "-O3", "-std=c++17", "-fPIC", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
         if src.endswith(".hip"):
@@ -35,7 +36,10 @@ def _library(lib: str, sources, verbose: bool) -> str:
             cmd += ["-x", "c++", "-D__HIP_PLATFORM_AMD__", "-I", os.path.join(os.environ.get("ROCM_PATH", "/opt/rocm"), "include")]
         cmd += ["-c", os.path.join(CSRC, src), "-o", obj]
         _run(cmd, verbose)
-        objs.append(obj)
+        return obj
+
+    with ThreadPoolExecutor(max_workers=4) as pool:          # a compiler each
+        objs = list(pool.map(compile_one, sources))
     # the interface and nothing else: helpers with plain names would meet a program's own
     _run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-Wl,--version-script=" + os.path.join(CSRC, "exports.map"), "-o", lib] + objs, verbose)
     return lib

@@ -8,5 +8,6 @@ def __getattr__(name):
         from . import layers
 
         if hasattr(layers, name):
-            return getattr(layers, name)
+            value = globals()[name] = getattr(layers, name)              # asked for once
+            return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

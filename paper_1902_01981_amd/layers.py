@@ -74,10 +74,17 @@ def _check(status: int) -> None:
 _DTYPES = {torch.float32: CR_F32, torch.bfloat16: CR_BF16}
 
 
+# A call takes the host as long as its launch does (4 us) and what is marshalled here: these two without the objects that torch.cuda makes of them (0.1 us
+# in place of 3 for a stream).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _on_device(t, name: str) -> None:
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch tensor")
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+    device = t.get_device()                              # -1: not on a GPU
+    if device < 0 or device != _current_device():
         raise ValueError(f"{name} must live on the current GPU")
 
 
@@ -146,7 +153,10 @@ def _bounds(bounds):
 
 
 def _stream(stream) -> int:
-    return torch.cuda.current_stream().cuda_stream if stream is None else stream
+    """The stream of a call: the one given, else torch's current one."""
+    if stream is not None:
+        return stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(_current_device())
 
 
 def _workspace(workspace, nbytes: int, stream):
@@ -154,7 +164,7 @@ def _workspace(workspace, nbytes: int, stream):
     if nbytes == 0:
         return 0, 0, None
     if workspace is None:
-        if stream is not None and stream != torch.cuda.current_stream().cuda_stream:
+        if stream is not None and stream != _stream(None):
             raise ValueError("a call on another stream than torch's current one brings its own workspace")
         workspace = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
     else:

@@ -294,19 +294,21 @@ hipError_t launch_dropout_backward(const DropoutGradArgs &args, void *workspace,
     for (int r = 0; r < a.runs; r += Pieces::kRuns) {
         Pieces p;
         const int count = lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), a.shape.positions, length, &p);
+        float *sums = a.dbias ? a.dbias + int64_t(r) * a.shape.channels : nullptr;
+        const bool direct = one_each(p);
         if (count > 0) {
             // far fewer than the grid's second dimension takes: at most one for each wanted workgroup and run
             const dim3 grid(tiles_of(c), count);
             auto pick = [&](auto bf16, auto is_flat) {
                 constexpr bool B = decltype(bf16)::value, F = decltype(is_flat)::value;
                 (!a.dbias ? dropout_backward_kernel<B, F, true, false> : a.dx.p ? dropout_backward_kernel<B, F, true, true> : dropout_backward_kernel<B, F, false, true>)
-                    <<<grid, kThreads, 0, stream>>>(a, c, p, parts);
+                    <<<grid, kThreads, 0, stream>>>(a, c, p, direct ? sums : parts);
             };
             using Yes = std::true_type;
             using No = std::false_type;
             a.shape.bf16 ? flat ? pick(Yes(), Yes()) : pick(Yes(), No()) : flat ? pick(No(), Yes()) : pick(No(), No());
         }
-        if (a.dbias) launch_sum_pieces(parts, nullptr, a.shape.channels, p, beside, a.dbias + int64_t(r) * a.shape.channels, nullptr, stream);
+        if (sums && !direct) launch_sum_pieces(parts, nullptr, a.shape.channels, p, beside, sums, nullptr, stream);
     }
     return hipGetLastError();
 }

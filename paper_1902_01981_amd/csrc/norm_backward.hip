@@ -477,13 +477,20 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
         Pieces pieces;
         const int count = lay_out_pieces(a.bounds + r, std::min(Pieces::kRuns, a.runs - r), p.units_per_point, p.length, &pieces);
         const float *from_gamma = parts_gamma, *from_beta = parts_beta;
+        float *to_gamma = parts_gamma, *to_beta = parts_beta;
+        float *dgamma = a.dgamma ? a.dgamma + int64_t(r) * s.channels : nullptr, *dbeta = a.dbeta ? a.dbeta + int64_t(r) * s.channels : nullptr;
+        const bool direct = sums && !p.cut && one_each(pieces);
+        if (direct) {                                    // what is not wanted has its place in the workspace all the same
+            if (dgamma) to_gamma = dgamma;
+            if (dbeta) to_beta = dbeta;
+        }
         if (p.cut && sums) {                             // rows of all pieces lie in one table
             from_gamma += pieces.first[0] * s.channels;
             from_beta += pieces.first[0] * s.channels;
         } else if (p.cut) {
             break;
         } else if (count > 0 && p.rows.lanes) {
-            launch_norm_rows_backward(a, p.rows, pieces, count, parts_gamma, parts_beta, stream);
+            launch_norm_rows_backward(a, p.rows, pieces, count, to_gamma, to_beta, stream);
         } else if (count > 0) {
             const Tiling &t = p.t;
             if (t.deep) {
@@ -493,7 +500,7 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
                     with_activation(a.activation, [&](auto act) {
                         constexpr int B = bf16(), V = vec(), U = unit(), A = act();
                         (t.deep == 4 ? norm_deep_backward_kernel<B, V, U == V ? 4 : 2, U, A> : norm_deep_backward_kernel<B, V, 2, U, A>)
-                            <<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                            <<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, to_gamma, to_beta);
                     });
                 });
             } else with_types(s, a.groups, [&](auto bf16, auto vec, auto unit) {
@@ -501,14 +508,12 @@ hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStrea
                     const size_t columns = t.threads * vec() * sizeof(float);
                     const size_t lds = std::max((2 * t.threads * (vec() / unit()) + 2 * t.side * most_groups(t, a.groups)) * sizeof(float), columns);
                     with_activation(a.activation, [&](auto act) {
-                        norm_tile_backward_kernel<bf16(), vec(), k(), unit(), act()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, parts_gamma, parts_beta);
+                        norm_tile_backward_kernel<bf16(), vec(), k(), unit(), act()><<<dim3(count, t.tiles), t.threads, lds, stream>>>(a, t, pieces, to_gamma, to_beta);
                     });
                 });
             });
         }
-        if (sums)
-            launch_sum_pieces(from_gamma, from_beta, s.channels, pieces, beside, a.dgamma ? a.dgamma + int64_t(r) * s.channels : nullptr,
-                              a.dbeta ? a.dbeta + int64_t(r) * s.channels : nullptr, stream);
+        if (sums && !direct) launch_sum_pieces(from_gamma, from_beta, s.channels, pieces, beside, dgamma, dbeta, stream);
     }
     return hipGetLastError();
 }

@@ -47,6 +47,13 @@ inline int lay_out_pieces(const int64_t *bounds, int runs, int64_t per_point, in
     for (int r = 0; r < runs; ++r) out->piece[r + 1] = out->piece[r] + static_cast<int>((out->first[r + 1] - out->first[r] + length - 1) / length);
     return out->piece[runs];
 }
+// Whether every run is one piece: what its workgroup adds up is the run's sum already.
+inline bool one_each(const Pieces &p)
+{
+    for (int r = 0; r < p.runs; ++r)
+        if (p.piece[r] != r) return false;
+    return p.piece[p.runs] == p.runs;
+}
 // The most pieces of a batch that these bounds give.
 inline int64_t most_pieces(const int64_t *bounds, int runs, int64_t per_point, int64_t length)
 {

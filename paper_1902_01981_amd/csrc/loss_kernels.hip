@@ -344,18 +344,24 @@ __device__ __forceinline__ void join_block(Softmax &s, float (&lds)[2][kSliceThr
     join_lanes<kSliceThreads / 64>(s);
 }
 
-// parts[row of the batch][slice] = (c, S)
-template <bool BF16, int VEC> __global__ void __launch_bounds__(kSliceThreads) loss_slices_kernel(LossArgs a, int slice, f2 *parts)
+// parts[row of the batch][slice] = (c, S).  The targets' logits go to at_targets[row]: in the next kernel the gradient may have replaced them.
+template <bool BF16, int VEC> __global__ void __launch_bounds__(kSliceThreads) loss_slices_kernel(LossArgs a, int slice, f2 *parts, float *at_targets)
 {
     using T = typename Chunk<BF16, VEC>::element;
     __shared__ float lds[2][kSliceThreads / 64];
     const int nq = (a.classes + VEC - 1) / VEC, begin = blockIdx.x * slice;
     Softmax s = add_slice<BF16, VEC>(a, static_cast<const T *>(a.logits) + blockIdx.y * a.row_stride, nq, begin, std::min(begin + slice, nq));
     join_block(s, lds);
-    if (threadIdx.x == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = f2{s.c, s.S};
+    if (threadIdx.x == 0) parts[int64_t(blockIdx.y) * gridDim.x + blockIdx.x] = f2{s.c, s.S};
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        RowTarget target;
+        read_target<false>(target, a, blockIdx.y);
+        read_logit<BF16, false>(target, a, blockIdx.y);
+        at_targets[blockIdx.y] = target.xt;
+    }
 }
 // Joins a row's slices, every workgroup for itself, and forms the gradient of its own slice.
-template <bool BF16, int VEC, bool GRAD> __global__ void __launch_bounds__(kSliceThreads) loss_join_kernel(LossArgs a, int slice, int slices, const f2 *parts)
+template <bool BF16, int VEC, bool GRAD> __global__ void __launch_bounds__(kSliceThreads) loss_join_kernel(LossArgs a, int slice, int slices, const f2 *parts, const float *at_targets)
 {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
@@ -363,7 +369,7 @@ template <bool BF16, int VEC, bool GRAD> __global__ void __launch_bounds__(kSlic
     const int64_t row = blockIdx.y;
     RowTarget target;
     read_target<true>(target, a, row);
-    read_logit<BF16, true>(target, a, row);
+    target.xt = scalar_load(at_targets + row);
     Softmax s;
     for (int i = threadIdx.x; i < slices; i += kSliceThreads) {
         const f2 p = parts[row * slices + i];
@@ -466,6 +472,7 @@ template <bool BF16> hipError_t launch(const LossArgs &a, const LossPlan &p, voi
     constexpr int VEC = BF16 ? 8 : 4;
     if (p.slices) {
         f2 *parts = static_cast<f2 *>(workspace);
+        float *at_targets = reinterpret_cast<float *>(parts + p.batch * p.per_row);
         constexpr int64_t e = BF16 ? 2 : 4;
         for (int64_t row = 0; row < a.rows; row += p.batch) {
             LossArgs b = a;
@@ -477,9 +484,9 @@ template <bool BF16> hipError_t launch(const LossArgs &a, const LossPlan &p, voi
             if (b.lse) b.lse += row;
             if (b.dlogits) b.dlogits = static_cast<char *>(a.dlogits) + row * a.dlogits_row_stride * e;
             const dim3 grid(p.per_row, static_cast<unsigned>(b.rows));
-            loss_slices_kernel<BF16, VEC><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, parts);
-            if (b.dlogits) loss_join_kernel<BF16, VEC, true><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts);
-            else loss_join_kernel<BF16, VEC, false><<<dim3(1, grid.y), kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts);
+            loss_slices_kernel<BF16, VEC><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, parts, at_targets);
+            if (b.dlogits) loss_join_kernel<BF16, VEC, true><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts, at_targets);
+            else loss_join_kernel<BF16, VEC, false><<<dim3(1, grid.y), kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts, at_targets);
         }
         return hipGetLastError();
     }
@@ -520,7 +527,7 @@ size_t loss_bytes(int64_t rows, int64_t classes, bool bf16)
 {
     if (rows == 0) return 0;
     const LossPlan p = plan_loss(rows, classes, bf16);
-    return p.slices ? static_cast<size_t>(p.batch * p.per_row) * sizeof(f2) : 0;
+    return p.slices ? static_cast<size_t>(p.batch) * (p.per_row * sizeof(f2) + sizeof(float)) : 0;
 }
 
 hipError_t launch_loss(const LossArgs &a, void *workspace, hipStream_t stream)

@@ -17,13 +17,6 @@ struct LayerShape {
     int positions, channels;
     bool bf16;
 };
-// A batch of runs of consecutive points as a kernel argument: run r of the batch is points [first[r], first[r + 1]).  Calls with more runs take
-// a launch per batch.
-struct RunTable {
-    static constexpr int kRuns = 256;
-    int runs;
-    int first[kRuns + 1];
-};
 
 struct NormArgs {
     LayerShape shape;

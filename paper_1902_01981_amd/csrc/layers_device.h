@@ -33,7 +33,6 @@ template <> struct Chunk<false, 1> {
     static __device__ __forceinline__ raw load(const element *p) { return *p; }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(p); }
     static __device__ __forceinline__ void store(element *p, raw r) { *p = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, p); }
     static __device__ __forceinline__ void widen(raw r, float (&v)[1]) { v[0] = r; }
     static __device__ __forceinline__ raw narrow(const float (&v)[1]) { return v[0]; }
 };
@@ -43,7 +42,6 @@ template <> struct Chunk<true, 1> {
     static __device__ __forceinline__ raw load(const element *p) { return *p; }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(p); }
     static __device__ __forceinline__ void store(element *p, raw r) { *p = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, p); }
     static __device__ __forceinline__ void widen(raw r, float (&v)[1]) { v[0] = __uint_as_float(static_cast<uint32_t>(r) << 16); }
     static __device__ __forceinline__ raw narrow(const float (&v)[1]) { return static_cast<raw>(pack_bf16(v[0], 0.f)); }
 };
@@ -54,7 +52,6 @@ template <> struct Chunk<false, 4> {
     static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
     static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(static_cast<memory>(r), reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
     static __device__ __forceinline__ raw narrow(const float (&v)[4]) { return raw{v[0], v[1], v[2], v[3]}; }
 };
@@ -65,7 +62,6 @@ template <> struct Chunk<true, 8> {
     static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
     static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
-    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(static_cast<memory>(r), reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[8])
     {
         v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);
@@ -138,19 +134,6 @@ template <int LANES> __device__ __forceinline__ float lanes_most(float v)
 {
     return fold_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
 }
-// The sum over a workgroup of T threads, for every thread; lds holds T / 64 floats and may be used again at once.
-template <int T> __device__ __forceinline__ float block_total(float v, float *lds)
-{
-    v = lanes_total<64>(v);
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < T / 64; ++w) v += lds[w];
-    __syncthreads();
-    return v;
-}
-
 // A pointer that is the same for all lanes, kept from being taken apart: what is added to it afterwards is the lane's offset of one access, not part
 // of an address per access that is held in registers throughout a loop.
 template <typename P> __device__ __forceinline__ P *scalar(P *p)

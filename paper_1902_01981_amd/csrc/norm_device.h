@@ -115,7 +115,7 @@ __device__ __forceinline__ Columns columns_of(const LayerShape &shape, int group
     return c;
 }
 
-// What a thread of a tile has: chunk `chunk` of the tile's columns (the last one moved back to end with them: the columns it shares with its neighbour come
+// What a thread of a tile has: a chunk of the tile's columns (the last one moved back to end with them: the columns it shares with its neighbour come
 // out the same in both), positions ty, ty + down, ... of point `side` of those side by side.
 struct Seat {
     int at, ty, side;            // at: channel in the tile
@@ -244,8 +244,7 @@ struct Parts {
     int stride;                  // most groups of a tile
     __device__ __forceinline__ int64_t at(const Tiling &t, int64_t point, int tile, int piece) const { return ((point * t.tiles + tile) * t.pieces + piece) * stride; }
 };
-// Folds f over the pieces (and slices) of every group of the tile; f(pair, values of the piece) per piece, by lanes that share a group.  Leaves F's
-// results in the tables `one` and `two`.
+// f(group, lane, lanes, first tile of the group) for every group of the tile, by lanes that share it and its pieces (and slices) between them.
 template <typename F> __device__ __forceinline__ void join_parts(const Parts &parts, const Tiling &t, const Columns &c, int64_t point, int tile, F f)
 {
     int lanes = 64;

@@ -319,7 +319,8 @@ inline void fold_columns(Tiling *t)
 // Tiles in registers: at most so many threads and chunks of each; k == 0: the point is too large, and is cut into pieces.  Small workgroups, of which
 // several share a compute unit and one loads while others add up; so tiles get more chunks of a thread, then narrower (down to a cache line of columns), and only
 // then more threads.  320 x 1 024 x 16 bf16 forward, 256 threads with 8 chunks each 11.5 us, 1 024 with two 17.0; 1 000 x 196 x 256 47 with 8 chunks, 70 with 4;
-// its gradient 96 with 8 chunks and 256 threads, 145 with 4 and 512, 112 in pieces.  Columns of half a line: 500 x 400 x 96 fp32 69 us, 55 with whole ones.
+// its gradient 96 with 8 chunks and 256 threads, 145 with 4 and 512, 112 in pieces.  Columns of half a line
+// rather than pieces: 500 x 400 x 96 fp32 gradient 110 us against 77 in pieces, 64 x 1 800 x 160 forward 74 against 43.
 inline Tiling tile(const LayerShape &s, int groups, bool backward)
 {
     // (the gradient of one position each leaves room for a group of 512 chunks)

@@ -6,7 +6,11 @@
 //
 //   loss_narrow_kernel   2 to 32 lanes per row
 //   loss_rows_kernel     a row in the registers of a wavefront or a workgroup, read once
-//   loss_slices_kernel, loss_join_kernel   rows wider than that, and a few wide rows: a row cut into slices, read twice
+//   loss_slices_kernel, loss_join_kernel   rows wider than that: a row cut into slices, read twice
+//
+// With the gradient, bf16, the reads and writes bound it: 32 768 x 4 096 83 us, 6.5 TB/s; 4 099 x 50 008 166 us, 4.9 TB/s; 8 192 x 131 072 817 us, 5.3 TB/s,
+// and 913 us, 4.7 TB/s, of 131 071 classes, whose rows begin anywhere.  Without it 32 768 x 4 096 43 us, 6.2 TB/s.  Narrow rows: 100 000 x 100 16 us,
+// 2.5 TB/s.  3 x 131 072 fp32 12.5 us, the launches.
 #include "layers_device.h"
 
 #include <algorithm>

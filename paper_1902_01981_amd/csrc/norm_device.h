@@ -328,7 +328,7 @@ inline Tiling tile(const LayerShape &s, int groups, bool backward)
     const int cg = s.channels / groups, line = std::max(1, 128 / (cg * (s.bf16 ? 2 : 4)));
     Tiling t = {};
     t.slices = t.unit = t.side = t.pieces = 1;
-    const int most_tiles = std::max(1, groups / line);
+    const int most_tiles = std::max(1, std::min(groups / line, 65535));      // of a grid's second dimension
     auto fits = [&](int threads, int chunks, int tiles) {
         const int across = across_for(s, groups, tiles);
         return across <= threads && ceil_div(groups, tiles) <= kMostGroups && int64_t(s.positions) <= int64_t(threads / across) * chunks;

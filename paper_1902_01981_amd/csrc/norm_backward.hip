@@ -11,7 +11,7 @@
 //   (points of one position: norm_rows.hip)
 //
 // Bound as the forward pass is, with twice the sums: 2 000 x 49 x 512 bf16, 32 groups, 90 us, 3.3 TB/s, two launches for 4 096 sums of a run among them;
-// 20 000 x 4 x 320 121 us, 1.3 TB/s.  Pieces are read twice, and the slopes of an activation formed twice: 64 x 4 096 x 512 bf16, 269 us, 5.0 TB/s of what
+// 20 000 x 4 x 320 69 us, 2.2 TB/s.  Pieces are read twice, and the slopes of an activation formed twice: 64 x 4 096 x 512 bf16, 269 us, 5.0 TB/s of what
 // moves, 3.0 of what has to.
 #include "norm_device.h"
 

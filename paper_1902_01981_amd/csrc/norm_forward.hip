@@ -10,8 +10,7 @@
 //   (points of one position: norm_rows.hip)
 //
 // Fewer than ten operations per byte, so the reads and writes are the floor.  A tile is bound by its chain of loads, sums and barriers, of which a compute
-// unit has a few at a time: 2 000 x 49 x 512 bf16, 32 groups, 45 us, 4.4 TB/s.  Of few positions more of the work is the sums and tables of the groups:
-// 20 000 x 4 x 320 bf16, 53 us, 1.9 TB/s.  Pieces are read twice: 64 x 4 096 x 512 bf16, 170 us, 4.7 TB/s of what moves, 3.2 of what has to.
+// unit has a few at a time: 2 000 x 49 x 512 bf16, 32 groups, 45 us, 4.4 TB/s.  20 000 x 4 x 320, 29 us, 3.5 TB/s.  Pieces are read twice: 64 x 4 096 x 512 bf16, 170 us, 4.7 TB/s of what moves, 3.2 of what has to.
 #include "norm_device.h"
 
 namespace cr {

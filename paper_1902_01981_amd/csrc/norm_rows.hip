@@ -6,7 +6,8 @@
 // comes out the same in both.
 //
 // The reads and writes bound it: 16 384 x 4 096 bf16, 32 groups, forward 49 us, 5.4 TB/s, gradient 80 us, 5.0 TB/s with the sums over the run after it;
-// 65 536 x 1 027 fp32, one group, 109 us, 4.9 TB/s, and 150 us, 5.4 TB/s.  (By workgroups that meet in LDS, as points of more positions: 167 and 1 243 us.)
+// 65 536 x 1 027 fp32, one group, 109 us, 4.9 TB/s, and 150 us, 5.4 TB/s.  (By workgroups that meet in
+// LDS, as points of more positions: 294 and 1 243 us.)
 #include "norm_device.h"
 
 namespace cr {

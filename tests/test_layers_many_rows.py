@@ -11,7 +11,7 @@ from test_layers_norm import _check_backward, _check_forward, _away_from_the_jum
 torch = pytest.importorskip("torch")
 
 # points, positions, channels, groups: several points of few positions to a thread, groups of whole loads, halves, quarters, odd; groups of 5 to 8 chunks a lane
-NORM = [(4100, 2, 640, 32), (4100, 2, 320, 10), (4200, 3, 300, 100), (4100, 1, 2004, 334), (2100, 1, 3000, 1), (2100, 1, 2999, 1), (2100, 4, 251, 1),
+NORM = [(4100, 2, 640, 32), (4100, 2, 320, 10), (4200, 3, 300, 100), (4100, 1, 2004, 334), (2100, 1, 3000, 1), (2100, 1, 2999, 1), (2100, 4, 251, 1), (2100, 5, 384, 128), (2100, 5, 387, 43), (4200, 17, 90, 2),
         (600, 20, 256, 32), (700, 1, 3001, 1), (300, 1, 1250, 1), (300, 1, 1501, 1), (300, 1, 1800, 1), (300, 1, 2040, 1), (300, 1, 2500, 1), (300, 1, 3500, 1),
         (300, 1, 4090, 1)]
 # a wavefront per row, twice around; workgroups of 8 and 16 chunks a thread

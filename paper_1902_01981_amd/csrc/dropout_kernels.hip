@@ -10,6 +10,7 @@
 // The reads and writes bound it where there are enough rows, 64 x 512 x 4 096 bf16: forward with residual 129 us, 6.2 TB/s, backward with the bias's
 // gradient 92 us, 5.8 TB/s; the two products of 64 bits per word hide behind them.  683 x 9 x 1 027 fp32, 12 runs: 11.8 us, 4.3 TB/s, and 18.1 us, 2.8 TB/s,
 // the second launch among them.  Small calls take what the host's part of a launch takes, 7 us.
+#include "row_step.h"
 #include "runs_device.h"
 
 namespace cr {
@@ -59,9 +60,9 @@ template <bool FLAT> struct RowWalk {
     {
         row.r += apart;
         if (!FLAT) {
-            const int position = row.position + positions_on, over = position >= positions;
-            row.point += points_on + over;
-            row.position = position - (over ? positions : 0);
+            const RowPlace to = row_place_on(RowPlace{row.point, row.position}, points_on, positions_on, positions);
+            row.point = to.point;
+            row.position = to.position;
         }
         return row;
     }

@@ -145,7 +145,8 @@ template <typename P> __device__ __forceinline__ P *scalar(P *p)
 // Says that a loaded value is needed from here on, so that its load is not moved behind a branch to where it is first used: several loads asked for together
 // stay together.
 template <typename R> __device__ __forceinline__ void hold(R &raw) { asm volatile("" : "+v"(raw)); }
-// A value at an address that is the same for all lanes, through the scalar cache: waiting for it is not waiting for vector loads.
+// A value at an address that is the same for all lanes, through the scalar cache: waiting for it is not waiting for vector loads.  For memory that nobody
+// writes while the kernel runs: the compiler takes it for constant.
 template <typename P> __device__ __forceinline__ P scalar_load(const P *p)
 {
     return *reinterpret_cast<const __attribute__((address_space(4))) P *>(reinterpret_cast<uintptr_t>(p));

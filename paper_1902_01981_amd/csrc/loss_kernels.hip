@@ -64,6 +64,8 @@ template <bool SCALAR> __device__ __forceinline__ void read_target(RowTarget &r,
     r.t = SCALAR ? scalar_load(a.targets + row) : a.targets[row];
     r.w = !a.weights ? 1.f : SCALAR ? scalar_load(a.weights + row) : a.weights[row];
 }
+// SCALAR only where no gradient is written: it may be written over the logits, and what is read through the scalar cache has to stay as it is while the
+// kernel runs, so that the compiler may read it late, or twice.
 template <bool BF16, bool SCALAR> __device__ __forceinline__ void read_logit(RowTarget &r, const LossArgs &a, int64_t row)
 {
     using E = Element<BF16>;
@@ -266,7 +268,7 @@ template <bool BF16, int K, bool WAVE, bool GRAD> __global__ void __launch_bound
     RowTarget now, next, after;
     read_target<true>(now, a, row);
     read_target<true>(next, a, std::min(row + stride, a.rows - 1));
-    read_logit<BF16, true>(now, a, row);
+    read_logit<BF16, !GRAD>(now, a, row);
     if constexpr (GRAD) {
 #pragma unroll
         for (int k = 0; k < K; ++k) add(k);
@@ -275,7 +277,7 @@ template <bool BF16, int K, bool WAVE, bool GRAD> __global__ void __launch_bound
             join();
             if (lane == 0) write_row(a, row, now, s);
             read_target<true>(after, a, std::min(row + 2 * stride, a.rows - 1));
-            read_logit<BF16, true>(next, a, row + stride);
+            read_logit<BF16, !GRAD>(next, a, row + stride);
             form(row, now, std::true_type(), row_at(row + stride));
             now = next;
             next = after;
@@ -291,7 +293,7 @@ template <bool BF16, int K, bool WAVE, bool GRAD> __global__ void __launch_bound
         for (; row < a.rows; row += stride) {
             x = row_at(row + stride);                    // past the last row: that row once more, from the caches
             read_target<true>(after, a, std::min(row + 2 * stride, a.rows - 1));
-            read_logit<BF16, true>(next, a, std::min(row + stride, a.rows - 1));
+            read_logit<BF16, !GRAD>(next, a, std::min(row + stride, a.rows - 1));
             s = Softmax();
 #pragma unroll
             for (int k = 0; k < K; ++k) {

@@ -108,6 +108,7 @@ int cr_dropout_backward(const cr_layer_shape_t *shape, const cr_layer_view_t *dy
  * Row by row, with x the row's logits, t its target and w its weight:
  *     lse = log(sum_j exp(x_j)),   loss = w (lse - x_t),   dlogits_j = w (exp(x_j - lse) - [j = t])
  * and the loss of a batch is their sum.
+ * The loss is formed from the logits' distances to the largest one, not from lse, so that it is as good beside large logits as beside small ones.
  *   logits    rows x classes of `dtype` (enum cr_xdtype), contiguous classes, row_stride elements apart
  *   targets   `rows` int64.  Negative: the row counts for nothing (loss and gradient 0, whatever its logits).  At least `classes`: no class;
  *             loss and gradient are NaN

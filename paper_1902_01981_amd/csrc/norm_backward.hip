@@ -19,38 +19,39 @@ namespace cr {
 
 namespace {
 
-// What a thread needs of its channels for the gradient.
-template <bool BF16, int VEC, int ACT> struct Gradient {
+// What a thread needs of its channels for the gradient.  x - mean stands for h where rstd can be multiplied in later, in sums and once per channel.  (Not
+// x rstd - mean rstd: where a group's values are close together the rounding of one product would be left over.)
+template <int VEC, int ACT> struct Gradient {
     float mean[VEC], rstd[VEC], gamma[VEC], beta[VEC];
-    __device__ __forceinline__ float h(float x, int v) const { return Normal<BF16>(mean[v], rstd[v])(x); }
-    // dz from dy; h is left in x
+    // dz from dy; x - mean is left in x
     __device__ __forceinline__ void slopes(float (&x)[VEC], float (&d)[VEC]) const
     {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-            x[v] = h(x[v], v);
-            d[v] = through_slope<ACT>(fmaf(x[v], gamma[v], beta[v]), d[v]);
+            x[v] -= mean[v];
+            d[v] = through_slope<ACT>(fmaf(x[v] * rstd[v], gamma[v], beta[v]), d[v]);
         }
     }
 };
-// dx = rstd (gamma dz - A - h B); where a group is one value gamma dz and A are the same, and nothing is left of them
+// dx = rstd (gamma dz - A - h B) from x - mean and dz; where a group is one value gamma dz and A are the same, and what is left of them is the rounding of
+// that product
 template <int VEC> struct Correction {
     float A[VEC], B[VEC];
-    __device__ __forceinline__ Correction(const float (&sum_A)[VEC], const float (&sum_B)[VEC], float share)
+    template <typename G> __device__ __forceinline__ Correction(const G &g, const float (&sum_A)[VEC], const float (&sum_B)[VEC], float share)
     {
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
             A[v] = sum_A[v] * share;
-            B[v] = sum_B[v] * share;
+            B[v] = sum_B[v] * share * g.rstd[v];
         }
     }
-    template <typename G> __device__ __forceinline__ float operator()(const G &g, float h, float dz, int v) const
+    template <typename G> __device__ __forceinline__ float operator()(const G &g, float from_mean, float dz, int v) const
     {
-        return g.rstd[v] * fmaf(-h, B[v], fmaf(g.gamma[v], dz, -A[v]));
+        return g.rstd[v] * fmaf(-from_mean, B[v], fmaf(g.gamma[v], dz, -A[v]));
     }
 };
 // mean and 1 / deviation of a seat's channels, from the tensors
-template <int VEC, int UNIT> __device__ __forceinline__ void read_stats(float (&m)[VEC], float (&r)[VEC], const NormGradArgs &a, const Seat &s, const Columns &c, int64_t point, int cg)
+template <int VEC, int UNIT, bool WAIT = false> __device__ __forceinline__ void read_stats(float (&m)[VEC], float (&r)[VEC], const NormGradArgs &a, const Seat &s, const Columns &c, int64_t point, int cg)
 {
     const float *mean = a.mean + point * a.groups + c.group, *rstd = a.rstd + point * a.groups + c.group;
     Columns one = c;
@@ -59,11 +60,11 @@ template <int VEC, int UNIT> __device__ __forceinline__ void read_stats(float (&
     seat.side = 0;
     const int within = c.first - c.group * cg;           // a slice of a group begins inside it
     seat.at += within;
-    spread<VEC, UNIT>(m, mean, seat, one, cg);
-    spread<VEC, UNIT>(r, rstd, seat, one, cg);
+    spread<VEC, UNIT, WAIT>(m, mean, seat, one, cg);
+    spread<VEC, UNIT, WAIT>(r, rstd, seat, one, cg);
 }
 
-// The groups' sums of gamma s1 and gamma s2, for every thread.
+// The groups' sums of gamma s1 and gamma s2, s1 over dz and s2 over dz h, for every thread.
 template <int VEC, int UNIT>
 __device__ __forceinline__ void bring(GroupSum<VEC, UNIT> &sums, const Seat &s, const float (&gamma)[VEC], float (&s1)[VEC], float (&s2)[VEC], int room, float *A_of, float *B_of)
 {
@@ -95,7 +96,7 @@ __global__ void __launch_bounds__(K == 1 ? 512 : 256) norm_tile_backward_kernel(
     const int room = t.threads * (VEC / UNIT);
     float *A_of = lds + 2 * room, *B_of = A_of + t.side * c.groups;
     const float share = 1.f / (static_cast<float>(positions) * cg);
-    Gradient<BF16, VEC, ACT> g;
+    Gradient<VEC, ACT> g;
     float sum_gamma[VEC], sum_beta[VEC];
     read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(g.beta, a.beta, c.first + s.at, 0.f);
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(K == 1 ? 512 : 256) norm_tile_backward_kernel(
             raw[k] = C::load_once(x.at_or_first(k, exists(s.ty, k, t.down, positions)));
             raw_d[k] = C::load_once(dy.at_or_first(k, exists(s.ty, k, t.down, positions)));
         }
-        read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, n, cg);
+        read_stats<VEC, UNIT, true>(g.mean, g.rstd, a, s, c, n, cg);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             hold(raw[k]);
@@ -136,6 +137,8 @@ __global__ void __launch_bounds__(K == 1 ? 512 : 256) norm_tile_backward_kernel(
                 }
             }
         }
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) s2[v] *= g.rstd[v];
         if (live) {
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
@@ -149,7 +152,7 @@ __global__ void __launch_bounds__(K == 1 ? 512 : 256) norm_tile_backward_kernel(
             float A[VEC], B[VEC];
             spread<VEC, UNIT>(A, A_of, s, c, cg);
             spread<VEC, UNIT>(B, B_of, s, c, cg);
-            const Correction<VEC> dx_of(A, B, share);
+            const Correction<VEC> dx_of(g, A, B, share);
             const Walk<BF16, VEC> dx(a.dx, n, s.ty, c.first + s.at, t.down);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -157,7 +160,7 @@ __global__ void __launch_bounds__(K == 1 ? 512 : 256) norm_tile_backward_kernel(
                     float h[VEC];
                     C::widen(raw[k], h);
 #pragma unroll
-                    for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, g.h(h[v], v), dz[k][v], v);
+                    for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, h[v] - g.mean[v], dz[k][v], v);
                     C::store(dx.at(k), C::narrow(h));
                 }
             }
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(512) norm_deep_backward_kernel(NormGradArgs a,
     float *A_of = lds + 2 * K * room, *B_of = A_of + K * tables;
     const float share = 1.f / (static_cast<float>(positions) * cg);
     const bool there = s.ty < positions;
-    Gradient<BF16, VEC, ACT> g;
+    Gradient<VEC, ACT> g;
     float sum_gamma[VEC], sum_beta[VEC];
     read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(g.beta, a.beta, c.first + s.at, 0.f);
@@ -220,6 +223,7 @@ __global__ void __launch_bounds__(512) norm_deep_backward_kernel(NormGradArgs a,
 #pragma unroll
             for (int v = 0; v < VEC; ++v) {
                 s1[v] = counts ? dz[k][v] : 0.f;
+                h[v] *= g.rstd[v];
                 s2[v] = s1[v] * h[v];
                 sum_beta[v] += s1[v];
                 sum_gamma[v] = fmaf(s1[v], h[v], sum_gamma[v]);
@@ -245,9 +249,9 @@ __global__ void __launch_bounds__(512) norm_deep_backward_kernel(NormGradArgs a,
                 spread<VEC, UNIT>(A, A_of + k * tables, s, c, cg);
                 spread<VEC, UNIT>(B, B_of + k * tables, s, c, cg);
                 read_stats<VEC, UNIT>(g.mean, g.rstd, a, s, c, point(k), cg);
-                const Correction<VEC> dx_of(A, B, share);
+                const Correction<VEC> dx_of(g, A, B, share);
 #pragma unroll
-                for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, g.h(h[v], v), dz[k][v], v);
+                for (int v = 0; v < VEC; ++v) h[v] = dx_of(g, h[v] - g.mean[v], dz[k][v], v);
                 const Walk<BF16, VEC> dx(a.dx, point(k), s.ty, c.first + s.at, t.down);
                 C::store(dx.base + dx.offset, C::narrow(h));
             }
@@ -279,7 +283,7 @@ __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a,
     float *A_of = lds + 2 * room, *B_of = A_of + c.groups;
     const Stretch stretch = stretch_of(t, piece, s.ty, a.shape.positions);
     Walk<BF16, VEC> x(a.x, n, stretch.first, c.first + s.at, t.down), dy(a.dy, n, stretch.first, c.first + s.at, t.down);
-    Gradient<BF16, VEC, ACT> g;
+    Gradient<VEC, ACT> g;
     float s1[VEC], s2[VEC];
     read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(g.beta, a.beta, c.first + s.at, 0.f);
@@ -306,6 +310,8 @@ __global__ void __launch_bounds__(256) norm_part_backward_kernel(NormGradArgs a,
             }
         }
     }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) s2[v] *= g.rstd[v];
     if (parts_gamma) {
         auto give = [&](float *to) { return [=](int col, float total) { to[int64_t(blockIdx.x) * a.shape.channels + c.first + col] = total; }; };
         add_columns(s2, s.has, s.at, s.ty, t.down, c.width, lds, give(parts_gamma));
@@ -348,7 +354,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
             B_of[g] = static_cast<float>(sum_B / all);
         }
     });
-    Gradient<BF16, VEC, ACT> g;
+    Gradient<VEC, ACT> g;
     float A[VEC], B[VEC];
     read_floats(g.gamma, a.gamma, c.first + s.at, 1.f);
     read_floats(g.beta, a.beta, c.first + s.at, 0.f);
@@ -358,7 +364,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
     const int cg_tile = t.slices == 1 ? cg : c.width;
     spread<VEC, UNIT>(A, A_of, s, c, cg_tile);
     spread<VEC, UNIT>(B, B_of, s, c, cg_tile);
-    const Correction<VEC> dx_of(A, B, 1.f);
+    const Correction<VEC> dx_of(g, A, B, 1.f);
     for (int left = stretch.left; left > 0; left -= U) {
         hold_step(raw);
         hold_step(raw_d);

@@ -57,8 +57,8 @@ __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::ra
     sums(s, sum, m2);
 }
 
-// y from x: gamma h + beta and the activation; by one multiply-add from bf16, as Normal
-template <bool BF16, int VEC, int ACT> struct Finish {
+// y from x: gamma h + beta and the activation
+template <int VEC, int ACT> struct Finish {
     float shift[VEC], scale[VEC], beta[VEC];
     __device__ __forceinline__ Finish(const NormArgs &a, int channel, const float (&mean)[VEC], const float (&rstd)[VEC])
     {
@@ -68,13 +68,12 @@ template <bool BF16, int VEC, int ACT> struct Finish {
         for (int v = 0; v < VEC; ++v) {
             scale[v] *= rstd[v];
             shift[v] = mean[v];
-            if (BF16) beta[v] = fmaf(-mean[v], scale[v], beta[v]);
         }
     }
     __device__ __forceinline__ void operator()(float (&x)[VEC]) const
     {
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) x[v] = activated<ACT>(fmaf(BF16 ? x[v] : x[v] - shift[v], scale[v], beta[v]));
+        for (int v = 0; v < VEC; ++v) x[v] = activated<ACT>(fmaf(x[v] - shift[v], scale[v], beta[v]));
     }
 };
 
@@ -110,7 +109,7 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT, int MOST> __global__ voi
             float m[VEC], r[VEC];
             spread<VEC, UNIT>(m, mean, s, c, cg);
             spread<VEC, UNIT>(r, rstd, s, c, cg);
-            const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+            const Finish<VEC, ACT> finish(a, c.first + s.at, m, r);
             const Walk<BF16, VEC> y(a.y, n, s.ty, c.first + s.at, t.down);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -138,7 +137,9 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT> __global__ void __launch
     GroupSum<VEC, UNIT> sums = {lds, t, c, cg};
     const int room = t.threads * NV, tables = t.side * c.groups;
     float *mean = lds + K * room, *rstd = mean + K * tables;
-    const float count = static_cast<float>(positions) * cg, share = 1.f / count;
+    // in scalar registers: one more vector register would cost a wavefront a unit
+    auto scalar_of = [](float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); };
+    const float count = scalar_of(static_cast<float>(positions) * cg), share = scalar_of(1.f / count);
     const bool there = s.ty < positions;
     for (int64_t n0 = int64_t(blockIdx.x) * t.side * K; n0 < a.shape.points; n0 += int64_t(gridDim.x) * t.side * K) {
         const int64_t n = n0 + s.side;                   // and n + side, ...
@@ -166,7 +167,7 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT> __global__ void __launch
             spread<VEC, UNIT>(m, mean + k * tables, s, c, cg);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                v[i] = fmaf(-m[i], share, v[i]);
+                v[i] -= quotient(m[i], count, share);
                 v[i] *= v[i];
             }
             gather<VEC, UNIT>(brought, v);
@@ -178,7 +179,7 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT> __global__ void __launch
         sums.add(lds, rstd, K, room);
         __syncthreads();
         for (int q = threadIdx.x; q < K * tables; q += blockDim.x) {
-            mean[q] *= share;
+            mean[q] = quotient(mean[q], count, share);
             rstd[q] = 1.f / sqrtf(fmaf(rstd[q], share, a.eps));
             const int64_t point = n0 + q / c.groups;     // tables of points n0, n0 + 1, ...
             if (a.mean && point < a.shape.points) {
@@ -193,7 +194,7 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT> __global__ void __launch
                 float v[VEC], m[VEC], r[VEC];
                 spread<VEC, UNIT>(m, mean + k * tables, s, c, cg);
                 spread<VEC, UNIT>(r, rstd + k * tables, s, c, cg);
-                const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+                const Finish<VEC, ACT> finish(a, c.first + s.at, m, r);
                 C::widen(raw[k], v);
                 finish(v);
                 const Walk<BF16, VEC> y(a.y, n + k * t.side, s.ty, c.first + s.at, t.down);
@@ -239,12 +240,12 @@ template <bool BF16, int VEC, int UNIT> __global__ void __launch_bounds__(256) n
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum[i / UNIT] += v[u][i];
             }
-            const float fresh = static_cast<float>(rows * UNIT), share = 1.f / fresh, total = have + fresh;
+            const float fresh = static_cast<float>(rows * UNIT), total = have + fresh;
             const float part = fresh / total;
             const float weight = have * part;
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const float m = sum[i] * share, apart = m - mean[i];
+                const float m = all() ? sum[i] * (1.f / (U * UNIT)) : sum[i] / fresh, apart = m - mean[i];          // the first is exact: a power of two
                 float q = 0.f;
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -328,7 +329,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
     const int cg_tile = t.slices == 1 ? cg : c.width;
     spread<VEC, UNIT>(m, mean, s, c, cg_tile);
     spread<VEC, UNIT>(r, rstd, s, c, cg_tile);
-    const Finish<BF16, VEC, ACT> finish(a, c.first + s.at, m, r);
+    const Finish<VEC, ACT> finish(a, c.first + s.at, m, r);
     for (int left = stretch.left; left > 0; left -= U) {
         hold_step(raw);
 #pragma unroll

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) norm_rows_forward_kernel(NormArgs a, int 
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) sum += lane.counts(k, i) ? v[k][i] : 0.f;
             }
-            const float mean = lanes_total<LANES>(sum) * share;
+            const float mean = quotient(lanes_total<LANES>(sum), static_cast<float>(cg), share);
             sum = 0.f;
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k)
@@ -157,7 +157,6 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t n = n0 + u * down;
-                const Normal<BF16> normal(mean[u], rstd[u]);
                 float h[CHUNKS][VEC], d[CHUNKS][VEC], A = 0.f, B = 0.f;
 #pragma unroll
                 for (int k = 0; k < CHUNKS; ++k) {
@@ -165,7 +164,7 @@ __global__ void __launch_bounds__(256) norm_rows_backward_kernel(NormGradArgs a,
                     C::widen(raw_d[u][k], d[k]);
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) {
-                        h[k][i] = normal(h[k][i]);
+                        h[k][i] = (h[k][i] - mean[u]) * rstd[u];
                         d[k][i] = through_slope<ACT>(fmaf(h[k][i], gamma[k][i], beta[k][i]), d[k][i]);
                         const float t = lane.counts(k, i) ? gamma[k][i] * d[k][i] : 0.f;
                         A += t;

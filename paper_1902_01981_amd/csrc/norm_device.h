@@ -37,7 +37,7 @@ template <int ACT> __device__ __forceinline__ float through_slope(float z, float
     return d;
 }
 // sum / count with share = 1 / count rounded: the product, and what it leaves of the sum.  An exact sum's mean is exact if 32 bits hold it, so that equal values
-// have no distance from it that a large rstd would show.
+// have no distance from it that a large rstd would show; an infinite sum's is NaN.
 __device__ __forceinline__ float quotient(float sum, float count, float share)
 {
     const float q = sum * share;

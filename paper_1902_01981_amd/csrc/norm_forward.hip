@@ -17,6 +17,9 @@ namespace cr {
 
 namespace {
 
+// The mean of a group as its user gets it: not an infinity, which is what a group with one in it may have for a mean (its rstd is NaN then).
+__device__ __forceinline__ float known(float mean, float rstd) { return rstd != rstd ? rstd : mean; }
+
 // The mean and the sum of squared distances from it, for the groups of a tile: mean[side * groups + group], M2 likewise.
 template <bool BF16, int VEC, int K, int UNIT>
 __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::raw (&raw)[K], const Seat &s, int positions, const Tiling &t, const Columns &c, int cg,
@@ -100,7 +103,7 @@ template <bool BF16, int VEC, int K, int UNIT, int ACT, int MOST> __global__ voi
             rstd[q] = 1.f / sqrtf(rstd[q] / count + a.eps);
             const int64_t point = n0 + q / c.groups;
             if (a.mean && point < a.shape.points) {
-                a.mean[point * a.groups + c.group + q % c.groups] = mean[q];
+                a.mean[point * a.groups + c.group + q % c.groups] = known(mean[q], rstd[q]);
                 a.rstd[point * a.groups + c.group + q % c.groups] = rstd[q];
             }
         }
@@ -318,7 +321,7 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
             mean[g] = static_cast<float>(m);
             rstd[g] = 1.f / sqrtf(static_cast<float>(sum / all) + a.eps);
             if (a.mean && piece == 0 && tile == first_tile) {
-                a.mean[n * a.groups + c.group + g] = mean[g];
+                a.mean[n * a.groups + c.group + g] = known(mean[g], rstd[g]);
                 a.rstd[n * a.groups + c.group + g] = rstd[g];
             }
         }

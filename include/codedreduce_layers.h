@@ -40,7 +40,8 @@ typedef struct cr_layer_shape {
     int32_t dtype;                       /* enum cr_xdtype of the activations */
 } cr_layer_shape_t;
 
-typedef struct cr_layer_view {           /* element (n, p, c) is at dev + (n * point_stride + p * position_stride + c) elements */
+typedef struct cr_layer_view {           /* element (n, p, c) is at dev + (n * point_stride + p * position_stride + c) elements; strides up to 2^40, */
+                                         /* points * point_stride + positions * position_stride + channels up to 2^60 */
     void *dev;
     int64_t point_stride, position_stride;
 } cr_layer_view_t;

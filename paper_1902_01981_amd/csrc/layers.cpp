@@ -53,6 +53,9 @@ int read_view(const cr_layer_view_t *view, const cr::LayerShape &shape, bool out
     int64_t point = shape.points > 1 ? view->point_stride : 0, position = shape.positions > 1 ? view->position_stride : 0;
     constexpr int64_t kMost = int64_t(1) << 40;
     if (point < 0 || position < 0 || point > kMost || position > kMost) return fail(CR_E_INVAL, name, ": strides must be in 0 .. 2^40");
+    // the kernels' offsets, and the sums below, have 64 bits; strides and counts can each be what they may and their products more
+    if (static_cast<__int128>(shape.points) * point + static_cast<__int128>(shape.positions) * position + shape.channels > int64_t(1) << 60)
+        return fail(CR_E_INVAL, name, " reaches past any address");
     if (output) {                                        // rows beside each other, the dimension of the smaller stride inside the other
         const bool points_outside = shape.points == 1 || (shape.positions == 1 ? true : point >= position);
         const int64_t inner = points_outside ? position : point, inner_count = points_outside ? shape.positions : shape.points;

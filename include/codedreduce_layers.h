@@ -68,7 +68,9 @@ const char *cr_layers_last_error(void);
  *   dx            may be dy or x itself; NULL: not wanted
  *   dgamma, dbeta runs x channels floats each; NULL: not wanted (each by itself)
  * act' of CR_ACT_RELU is 0 at 0.
- * cr_group_norm_workspace_bytes: what a call on this shape needs (256-byte aligned), whichever strides and pointers it has; may be 0. */
+ * cr_group_norm_workspace_bytes: what a call on this shape needs (256-byte aligned), whichever strides and pointers it has; may be 0.
+ * A point that no workgroup holds is cut into pieces of 2 000 values or more.  Points with 2^31 pieces between them (4 * 10^12 values or more: inputs that
+ * are broadcast) are refused by cr_group_norm_workspace_bytes and cr_group_norm_backward. */
 int cr_group_norm_workspace_bytes(const cr_layer_shape_t *shape, int groups, const int64_t *bounds, int runs, size_t *forward_bytes,
                                   size_t *backward_bytes);
 int cr_group_norm_forward(const cr_layer_shape_t *shape, const cr_layer_view_t *x, const float *gamma, const float *beta, int groups,

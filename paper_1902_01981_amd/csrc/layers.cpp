@@ -85,6 +85,11 @@ int check_activation(int activation)
     return activation >= CR_ACT_NONE && activation <= CR_ACT_SILU ? CR_OK : fail(CR_E_INVAL, "activation", " is unknown");
 }
 
+int check_pieces(const cr::LayerShape &shape, int groups)
+{
+    return cr::norm_backward_numbered(shape, groups) ? CR_OK : fail(CR_E_INVAL, "points, positions", " are too many together for a gradient");
+}
+
 // The runs' bounds as they are, or one run of all points in `whole`.
 int read_bounds(const cr::LayerShape &shape, const int64_t *bounds, int runs, int64_t (&whole)[2], const int64_t **out)
 {
@@ -138,6 +143,7 @@ int cr_group_norm_workspace_bytes(const cr_layer_shape_t *shape, int groups, con
     CR_TRY(read_shape(shape, &s));
     CR_TRY(check_groups(s, groups));
     CR_TRY(read_bounds(s, bounds, runs, whole, &b));
+    CR_TRY(check_pieces(s, groups));
     if (!forward_bytes || !backward_bytes) return fail(CR_E_INVAL, "forward_bytes, backward_bytes", " are required");
     *forward_bytes = cr::norm_forward_bytes(s, groups);
     *backward_bytes = cr::norm_backward_bytes(s, groups, b, runs);
@@ -175,6 +181,7 @@ int cr_group_norm_backward(const cr_layer_shape_t *shape, const cr_layer_view_t 
     CR_TRY(check_groups(a.shape, groups));
     CR_TRY(check_activation(activation));
     CR_TRY(read_bounds(a.shape, bounds, runs, whole, &a.bounds));
+    CR_TRY(check_pieces(a.shape, groups));
     CR_TRY(check_floats(gamma, false, "gamma"));
     CR_TRY(check_floats(beta, false, "beta"));
     CR_TRY(check_floats(dgamma, false, "dgamma"));

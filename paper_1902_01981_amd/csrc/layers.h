@@ -37,6 +37,7 @@ struct NormGradArgs {
     float *dgamma, *dbeta;                               // or null
 };
 size_t norm_forward_bytes(const LayerShape &shape, int groups);
+bool norm_backward_numbered(const LayerShape &shape, int groups);       // whether 32 bits number the pieces that leave sums
 size_t norm_backward_bytes(const LayerShape &shape, int groups, const int64_t *bounds, int runs);
 hipError_t launch_norm_forward(const NormArgs &a, void *workspace, hipStream_t stream);
 hipError_t launch_norm_backward(const NormGradArgs &a, void *workspace, hipStream_t stream);

@@ -443,6 +443,11 @@ BackwardRoom room_of(const LayerShape &s, int groups, const BackwardPlan &p, con
 
 }  // namespace
 
+bool norm_backward_numbered(const LayerShape &s, int groups)
+{
+    return s.points == 0 || s.points < (int64_t(1) << 31) / plan_backward(s, groups).units_per_point;
+}
+
 size_t norm_backward_bytes(const LayerShape &s, int groups, const int64_t *bounds, int runs)
 {
     return s.points == 0 ? 0 : room_of(s, groups, plan_backward(s, groups), bounds, runs).bytes();

@@ -1,4 +1,6 @@
 """Views whose strides are allowed one by one, but together reach past what an offset of 64 bits can say: refused, not wrapped around.  (No launch follows.)"""
+import ctypes
+
 import pytest
 
 import paper_1902_01981_amd as cr
@@ -46,3 +48,23 @@ def test_what_overlaps_by_one_element_at_the_border():
         status = cr.load_layers_library().cr_group_norm_backward(shape(n, p, c, cr.CR_BF16), layers.cr_layer_view_t(HERE, 0, 0), layers.cr_layer_view_t(HERE, 0, 0), HERE,
                                                                  HERE, 0, 0, 1, 0, None, 1, layers.cr_layer_view_t(HERE, point, 1 << 12), 0, 0, 0, 0, 0)
         _refused(status, text or "workspace")            # what is right comes to a missing workspace
+
+
+def _gradient_bytes(points, positions, channels=1, dtype=cr.CR_BF16):
+    f, b = ctypes.c_size_t(), ctypes.c_size_t()
+    status = cr.load_layers_library().cr_group_norm_workspace_bytes(layers.cr_layer_shape_t(points, positions, channels, dtype), 1, 0, 1, ctypes.byref(f), ctypes.byref(b))
+    return status, b.value
+
+
+def test_pieces_of_points():
+    """Points cut into pieces leave a row of sums per piece.  Below 2^31 of them the workspace holds them all, above the gradient is refused (inputs that are
+    broadcast can be so large)."""
+    for points, positions in ((1 << 10, 1 << 16), (1 << 20, 1 << 20), (1 << 24, 1 << 19)):
+        status, nbytes = _gradient_bytes(points, positions)
+        pieces = points * positions // (256 * 64)        # threads of a workgroup, most positions of a thread
+        assert status == cr.CR_OK and nbytes >= 2 * 4 * pieces
+    _refused(_gradient_bytes(1 << 24, 1 << 24)[0], "points")
+    _refused(_gradient_bytes((1 << 31) - 1, (1 << 31) - 1)[0], "points")
+    view, lib = layers.cr_layer_view_t(HERE, 0, 0), cr.load_layers_library()
+    _refused(lib.cr_group_norm_backward(layers.cr_layer_shape_t(1 << 24, 1 << 24, 1, cr.CR_BF16), view, view, HERE, HERE, 0, 0, 1, 0, None, 1, None, HERE, HERE, 0, 0, 0),
+             "points")

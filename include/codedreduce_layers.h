@@ -2,7 +2,8 @@
  *
  * Coded aggregation (codedreduce.h) recovers the exact full gradient from what redundant workers form, on three conditions on the network
  * whose gradients are handed to it: its loss is a SUM over data points; a point's gradient depends on that point alone, whatever else its
- * holder has; and every holder of a point forms the same gradient.  These are the layers of a network that keep them:
+ * holder has; and every holder of a point forms the same gradient.  These are the layers of a network that keep them (the last up to
+ * rounding, as the conventions say):
  *
  *     cr_group_norm_*     normalisation within a data point, with an activation
  *     cr_dropout_*        dropout whose mask is a function of the data point's index, not of who draws it or when; with bias and residual
@@ -23,7 +24,9 @@
  *   - an output may be the very tensor of an input (same address, same strides) where this is said; other overlaps are errors that are
  *     not looked for.
  *   - sums, statistics and exponentials are held in 32 bits or more; a result is rounded once, to its type.  Every sum has a fixed order:
- *     the same call on the same inputs gives the same bits.
+ *     the same call on the same inputs gives the same bits.  Between calls that have a point among other points, a row of the loss and what
+ *     dropout makes of a point are the same bits too; what a group norm makes of it may differ by rounding, since the order of its sums goes
+ *     by the number of points, as it does for gradients of parameters.
  *   - no points: CR_OK, gradients of parameters are zero.
  */
 #ifndef CODEDREDUCE_LAYERS_H

@@ -388,42 +388,6 @@ template <bool BF16, int VEC, int UNIT, int ACT> __global__ void __launch_bounds
     }
 }
 
-// points of a piece: a workgroup's sums of the parameters' gradients are over so many that they are little beside what it reads
-int64_t points_of_piece(const LayerShape &s, const Tiling &t)
-{
-    const int64_t wanted = std::max<int64_t>(1, kUnits * 8 / t.tiles);
-    int64_t length = std::max<int64_t>((s.points + wanted - 1) / wanted, std::min<int64_t>(32 / std::min(s.positions, 32), (s.points + kUnits - 1) / kUnits));
-    const int at_once = t.side * std::max(t.deep, 1);
-    return std::max<int64_t>((length + at_once - 1) / at_once * at_once, 1);
-}
-
-struct BackwardPlan {
-    RowsPlan rows;
-    bool cut;                    // norm_part and norm_join
-    Tiling t;
-    int64_t units_per_point, length;                     // of the pieces
-};
-BackwardPlan plan_backward(const LayerShape &s, int groups)
-{
-    BackwardPlan p = {};
-    p.units_per_point = 1;
-    p.rows = rows_plan(s, groups, true);
-    if (p.rows.lanes) {
-        p.length = rows_piece(s, groups, p.rows);
-        return p;
-    }
-    p.t = tile(s, groups, true);
-    if (p.t.k) {
-        p.length = points_of_piece(s, p.t);
-        return p;
-    }
-    p.cut = true;
-    p.t = cut(s, groups);
-    p.units_per_point = p.t.pieces;
-    p.length = 1;
-    return p;
-}
-
 size_t align_up(size_t v) { return (v + 255) / 256 * 256; }
 
 // What a backward call keeps in its workspace: rows of the pieces' sums for dgamma and dbeta, rows beside them, pairs of sums of the groups.

@@ -44,8 +44,6 @@ __device__ __forceinline__ Team take_team(int lanes, int groups, int wide, int d
     t.group = min(t.group, groups - 1);
     return t;
 }
-constexpr int points_at_once(int chunks) { return chunks == 1 ? 4 : chunks == 2 ? 2 : 1; }
-
 template <bool BF16, int LANES, int CHUNKS, bool EXACT, int ACT>
 __global__ void __launch_bounds__(256) norm_rows_forward_kernel(NormArgs a, int wide, int down, int64_t length)
 {
@@ -231,32 +229,7 @@ template <typename F> void with_team(const LayerShape &s, int groups, const Rows
     }
 }
 
-// points of a workgroup: enough workgroups to fill the chip several times, and a few steps for each
-int64_t points_of_workgroup(const LayerShape &s, int groups, const RowsPlan &p, int workgroups_per_unit, int steps)
-{
-    const int64_t tiles = ceil_div(groups, p.wide), step = p.down * points_at_once(p.chunks);
-    int64_t length = (s.points * tiles + kUnits * workgroups_per_unit - 1) / (kUnits * workgroups_per_unit);
-    length = (length + step - 1) / step * step;
-    return std::max<int64_t>({1, length, std::min(step * steps, (s.points + step - 1) / step * step)});
-}
-
 }  // namespace
-
-// The gradient of more channels than 32 a lane is more than the registers hold beside the sums for gamma and beta.
-RowsPlan rows_plan(const LayerShape &s, int groups, bool backward)
-{
-    const int vec = s.bf16 ? 8 : 4, cg = s.channels / groups, chunks = ceil_div(cg, vec);
-    RowsPlan p = {};
-    if (s.positions != 1 || cg < vec || chunks > 64 * (backward && s.bf16 ? 4 : 8)) return p;
-    p.lanes = 1;
-    while (p.lanes < 64 && p.lanes < chunks) p.lanes *= 2;
-    p.chunks = ceil_div(chunks, p.lanes);
-    const int teams = 256 / p.lanes;
-    p.wide = ceil_div(groups, ceil_div(groups, teams));
-    p.down = teams / p.wide;
-    return p;
-}
-int64_t rows_piece(const LayerShape &s, int groups, const RowsPlan &p) { return points_of_workgroup(s, groups, p, 4, 4); }
 
 void launch_norm_rows_forward(const NormArgs &a, const RowsPlan &p, hipStream_t stream)
 {

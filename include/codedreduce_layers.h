@@ -72,7 +72,9 @@ const char *cr_layers_last_error(void);
  *   dgamma, dbeta runs x channels floats each; NULL: not wanted (each by itself)
  * act' of CR_ACT_RELU is 0 at 0.
  * cr_group_norm_workspace_bytes: what a call on this shape needs (256-byte aligned), whichever strides and pointers it has; may be 0.
- * A point that no workgroup holds is cut into pieces of 2 000 values or more.  Points with 2^31 pieces between them (4 * 10^12 values or more: inputs that
+ * A point that no workgroup holds is cut into pieces of 2 000 values or more, and in the gradient every piece leaves 8 bytes a channel there.
+ * That is little beside the activations but for points of few positions and wide groups: of one position and more than 4 096 channels a group
+ * (2 048 of fp32), or of two to eight and half as many, it is 8 bytes a channel and point (16 384 points of 8 192 channels: 1.1 GB).  Points with 2^31 pieces between them (4 * 10^12 values or more: inputs that
  * are broadcast) are refused by cr_group_norm_workspace_bytes and cr_group_norm_backward. */
 int cr_group_norm_workspace_bytes(const cr_layer_shape_t *shape, int groups, const int64_t *bounds, int runs, size_t *forward_bytes,
                                   size_t *backward_bytes);

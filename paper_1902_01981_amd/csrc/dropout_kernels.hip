@@ -8,7 +8,7 @@
 //   sum_pieces_kernel      the bias's gradient per run, where runs are more than a piece each
 //
 // The reads and writes bound it where there are enough rows, 64 x 512 x 4 096 bf16: forward with residual 129 us, 6.2 TB/s, backward with the bias's
-// gradient 92 us, 5.8 TB/s; the two products of 64 bits per word hide behind them.  683 x 9 x 1 027 fp32, 12 runs: 11.8 us, 4.3 TB/s, and 18.1 us, 2.8 TB/s,
+// gradient 92 us, 5.8 TB/s; the two products of 64 bits per word hide behind them.  683 x 9 x 1 027 fp32, 12 runs: 11.8 us, 4.3 TB/s, and 17.7 us, 2.9 TB/s,
 // the second launch among them.  Small calls take what the host's part of a launch takes, 7 us.
 #include "row_step.h"
 #include "runs_device.h"
@@ -50,7 +50,7 @@ template <bool FLAT> struct Row {
     int position;
 };
 // The rows of a thread, so many apart: one division at the start, an addition and a comparison each.  (20 000 points of 9 x 256 bf16 with
-// indices, forward 37.1 us and backward 46.2; with a division per row 38.8 and 49.6.)
+// indices, forward 37.0 us and backward 45.9; with a division per row 38.8 and 49.6.)
 template <bool FLAT> struct RowWalk {
     const Mask &mask;
     int positions, apart, points_on, positions_on;

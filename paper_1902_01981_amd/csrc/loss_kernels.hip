@@ -8,9 +8,10 @@
 //   loss_rows_kernel     a row in the registers of a wavefront or a workgroup, read once
 //   loss_slices_kernel, loss_join_kernel   rows wider than that: a row cut into slices, read twice
 //
-// With the gradient, bf16, the reads and writes bound it: 32 768 x 4 096 83 us, 6.5 TB/s; 4 099 x 50 008 166 us, 4.9 TB/s; 8 192 x 131 072 817 us, 5.3 TB/s,
-// and 913 us, 4.7 TB/s, of 131 071 classes, whose rows begin anywhere.  Without it 32 768 x 4 096 43 us, 6.2 TB/s.  Narrow rows: 100 000 x 100 16 us,
-// 2.5 TB/s.  3 x 131 072 fp32 12.5 us, the launches.
+// With the gradient, bf16, the reads and writes bound it: 32 768 x 4 096 82 us, 6.5 TB/s; 4 099 x 50 008 165 us, 5.0 TB/s; 8 192 x 131 072 817 us, 5.3 TB/s,
+// and 913 us, 4.7 TB/s, of 131 071 classes, whose rows begin anywhere.  fp32, 4 099 x 50 008: 330 us, 5.0 TB/s.  Without it 32 768 x 4 096 bf16 43 us, 6.2 TB/s.
+// Narrow rows: 100 000 x 100 bf16 16 us, 2.5 TB/s.  3 x 131 072 fp32 13 us, the launches.  Rows wider than the registers: 8 192 x 152 064 bf16 1.55 ms, 4 096 x
+// 128 000 fp32 1.26 ms, both 5.0 TB/s of what moves, 3.3 of what has to.
 #include "layers_device.h"
 
 #include <algorithm>
@@ -21,7 +22,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float infinity() { return __builtin_inff(); }
-__device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }       // flushes results below 2^-126 to 0
+// e^v for v <= 0, the distance from the largest logit: off by |v| + 2 units of 2^-24 of itself, by less than 3 of them of the largest share, whose v is 0.
+// Results below 2^-126 are 0.
+__device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
 
 // c = reference, S = sum; c is finite unless the part has nothing but -infinity (S = 0 then) or a +infinity (S is NaN then)
 struct Softmax {
@@ -154,7 +157,7 @@ template <bool BF16, int VEC, int TS, bool GRAD> __global__ void __launch_bounds
 // are added to the running sum as they arrive, and as soon as a chunk's gradient is stored its place takes the chunk of the team's next row, so that
 // reads go on while gradients are formed and written.  For that to be so, a wait for one chunk must not be a wait for all: there is no branch around a
 // load or a store of a chunk, and a step ends with the sum over the row that it has asked for, so that its waits are counted from its own loads and
-// stores.  8 192 x 131 072 bf16, a row per workgroup: 801 us, with waits for everything 1 006.
+// stores.  That took 8 192 x 131 072 bf16, a row per workgroup, from 1 006 us to 801 (817 with loads that suit rows of odd lengths, below).
 // `lanes` threads have chunks, lanes = ceil(whole / K), so that all but the last of a thread lie in the row; whoever has no chunk there forms the last
 // whole one again, with the same bits, and does not count it.  What is behind the chunks has a lane per element in the last wavefront.  (Chunks on
 // 16-byte boundaries, whatever the row starts on, are faster where rows have odd lengths, 8 192 x 131 071 bf16 351 us against 430 without and 913

@@ -10,9 +10,9 @@
 //   sum_parts_kernel, sum_pieces_kernel   the parameters' gradients per run
 //   (points of one position: norm_rows.hip)
 //
-// Bound as the forward pass is, with twice the sums: 2 000 x 49 x 512 bf16, 32 groups, 90 us, 3.3 TB/s, two launches for 4 096 sums of a run among them;
-// 20 000 x 4 x 320 69 us, 2.2 TB/s.  Pieces are read twice, and the slopes of an activation formed twice: 64 x 4 096 x 512 bf16, 269 us, 5.0 TB/s of what
-// moves, 3.0 of what has to.
+// Bound as the forward pass is, with twice the sums: 2 000 x 49 x 512 bf16, 32 groups, 95 us, 3.2 TB/s, two launches for 4 096 sums of a run among them;
+// 20 000 x 4 x 320 72 us, 2.1 TB/s.  Pieces are read twice, and the slopes of an activation formed twice: 64 x 4 096 x 512 bf16, 269 us, 5.0 TB/s of what
+// moves, 3.0 of what has to.  1 x 4 454 x 2 240: 54 us, 28 of them the second kernel, as in the forward pass.
 #include "norm_device.h"
 
 namespace cr {

@@ -10,7 +10,9 @@
 //   (points of one position: norm_rows.hip)
 //
 // Fewer than ten operations per byte, so the reads and writes are the floor.  A tile is bound by its chain of loads, sums and barriers, of which a compute
-// unit has a few at a time: 2 000 x 49 x 512 bf16, 32 groups, 45 us, 4.4 TB/s.  20 000 x 4 x 320, 29 us, 3.5 TB/s.  Pieces are read twice: 64 x 4 096 x 512 bf16, 170 us, 4.7 TB/s of what moves, 3.2 of what has to.
+// unit has a few at a time: 2 000 x 49 x 512 bf16, 32 groups, 46 us, 4.3 TB/s.  20 000 x 4 x 320, 29 us, 3.5 TB/s.  One group of more channels than norm_rows.hip takes has 1 024 threads
+// and a chunk each: 16 384 x 8 192 bf16 500 us, 1.1 TB/s.  Pieces are read twice: 64 x 4 096 x 512 bf16, 170 us, 4.7 TB/s of what moves, 3.2 of what has to; where
+// points are few, every workgroup adding up all pieces' moments before it goes on is most of it: 1 x 4 454 x 2 240, 37 us, 29 of them the second kernel.
 #include "norm_device.h"
 
 namespace cr {
@@ -60,7 +62,7 @@ __device__ __forceinline__ void tile_moments(const typename Chunk<BF16, VEC>::ra
     sums(s, sum, m2);
 }
 
-// y from x: gamma h + beta and the activation
+// y from x: gamma h + beta and the activation.  gamma rstd is one number, rounded by itself: half a unit of gamma h.
 template <int VEC, int ACT> struct Finish {
     float shift[VEC], scale[VEC], beta[VEC];
     __device__ __forceinline__ Finish(const NormArgs &a, int channel, const float (&mean)[VEC], const float (&rstd)[VEC])

@@ -75,9 +75,9 @@ inline void fold_columns(Tiling *t)
 
 // Tiles in registers: at most so many threads and chunks of each; k == 0: the point is too large, and is cut into pieces.  Small workgroups, of which
 // several share a compute unit and one loads while others add up; so tiles get more chunks of a thread, then narrower (down to a cache line of columns), and only
-// then more threads.  320 x 1 024 x 16 bf16 forward, 256 threads with 8 chunks each 11.5 us, 1 024 with two 17.0; 1 000 x 196 x 256 47 with 8 chunks, 70 with 4;
-// its gradient 96 with 8 chunks and 256 threads, 145 with 4 and 512, 112 in pieces.  Columns of half a line
-// rather than pieces: 500 x 400 x 96 fp32 gradient 110 us against 77 in pieces, 64 x 1 800 x 160 forward 74 against 43.
+// then more threads.  320 x 1 024 x 16 bf16 forward, 256 threads with 8 chunks each 11.8 us, 1 024 with two 17.0; 1 000 x 196 x 256 47 with 8 chunks, 59 with 4;
+// its gradient 102 with 8 chunks and 256 threads, 145 with 4 and 512, 112 in pieces.  Columns of half a line rather than pieces, a point's tiles as far apart in
+// the grid as there are points: 500 x 400 x 96 fp32 gradient 110 us against 77 in pieces, 64 x 1 800 x 160 forward 74 against 42.
 inline Tiling tile(const LayerShape &s, int groups, bool backward)
 {
     // (the gradient of one position each leaves room for a group of 512 chunks)
@@ -102,8 +102,8 @@ inline Tiling tile(const LayerShape &s, int groups, bool backward)
         while (int64_t(t.threads / t.across) * t.k < s.positions) t.k *= 2;
         // Where there are points enough, more chunks of a thread and more points side by side: a thread adds up its own rows of a group before it meets others,
         // and a step of a workgroup is that much more.  (Not where over two fifths of what a thread could have would be empty.)  Forward and gradient, us,
-        // with the fewest chunks and so: 20 000 x 4 x 320 bf16 53 and 121, 29 and 69; 45 575 x 17 x 90 241 and 333, 77 and 190; 4 096 x 16 x 33 fp32 12 and
-        // 33, 9 and 20.  Sums per channel of eight channels: the gradient's registers are full at four chunks (45 575 x 17 x 90 with eight: 247).
+        // with the fewest chunks and so: 20 000 x 4 x 320 bf16 54 and 121, 29 and 72; 45 575 x 17 x 90 246 and 336, 77 and 196; 4 096 x 16 x 33 fp32 12 and
+        // 32, 9 and 19.  Sums per channel of eight channels: the gradient's registers are full at four chunks (45 575 x 17 x 90 with eight: 247).
         const int values = vec / unit_of(cg, vec), side = t.threads / (t.across * ceil_div(s.positions, t.k)), fewest = t.k;
         for (int k = 2 * fewest; k <= (backward && values == 8 ? 4 : most_chunks) && k / 2 < s.positions; k *= 2) {
             const int more_side = t.threads / (t.across * ceil_div(s.positions, k));
@@ -154,6 +154,8 @@ inline Tiling cut(const LayerShape &s, int groups)
 }
 inline int most_groups(const Tiling &t, int groups) { return t.slices > 1 ? 1 : ceil_div(groups, t.tiles); }
 
+// (A piece is of one point: points of few positions whose groups are wide, as 16 384 of one position and 8 192 bf16 channels in one group, leave a row of sums
+// each in the gradient, 1.1 GB of them beside 268 MB of activations, and take 1 075 us where the reads and writes that have to be are 161.)
 // Points of a pair of launches: as many as a grid takes.  (Fewer, so that what is read twice comes from the last-level cache, cost more at the launches' ends
 // than they gain: 64 x 4 096 x 512 bf16, points of 96 MB at a time / of 192 / all: forward 213 / 196 / 176 us, backward 365 / 320 / 279.)
 inline int64_t batch_points(const LayerShape &s, const Tiling &t) { return std::max<int64_t>(1, std::min<int64_t>(s.points, (int64_t(1) << 22) / t.pieces)); }

@@ -146,9 +146,12 @@ def _bounds(bounds):
     """(address, runs, what keeps the address alive) of the runs' bounds."""
     if bounds is None:
         return 0, 1, None
-    b = np.ascontiguousarray(bounds, dtype=np.int64)
-    if b.ndim != 1 or b.size < 2:
+    given = np.asarray(bounds)
+    if given.ndim != 1 or given.size < 2:
         raise ValueError("bounds must be runs + 1 numbers")
+    if given.dtype.kind not in "iu" and not ((np.abs(given) < 2.0 ** 62).all() and (np.mod(given, 1) == 0).all()):
+        raise ValueError("bounds must be whole numbers")
+    b = np.ascontiguousarray(given, dtype=np.int64)
     return b.ctypes.data, b.size - 1, b
 
 

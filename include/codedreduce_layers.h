@@ -62,6 +62,7 @@ const char *cr_layers_last_error(void);
  *   mean, rstd    points x groups floats each, what the gradient needs; NULL (both) where none will be asked for
  *   eps           >= 0
  * A point with a NaN or an infinity in a group has NaN there (mean and rstd of that group included) and nowhere else.
+ * Distances from the mean of 10^18 and more have squares that 32 bits do not hold: rstd may be 0 there, and h with it.
  *
  * cr_group_norm_backward: from dy and what the forward pass was given and left,
  *     dz = dy act'(gamma h + beta),   dbeta = sum dz,   dgamma = sum dz h   (over the points of a run and their positions),

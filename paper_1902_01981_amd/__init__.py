@@ -4,7 +4,7 @@ from .api import *  # noqa: F401,F403
 
 
 def __getattr__(name):
-    if name.startswith(("cr_layer", "cr_group_norm_", "cr_dropout_", "cr_softmax_loss", "CR_ACT_", "LAYERS_", "load_layers")):
+    if name.startswith(("cr_layer", "cr_group_norm_", "cr_dropout_", "cr_softmax_loss", "cr_embedding_", "cr_log_probs", "cr_distill_loss", "CR_ACT_", "LAYERS_", "load_layers")):
         from . import layers
 
         if hasattr(layers, name):

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcodedreduce.so")
 SOURCES = ["gc_design.cpp", "tree_plan.cpp", "latency_model.cpp", "codedreduce.cpp", "kernels.hip"]
 LAYERS_LIB = os.path.join(HERE, "libcodedreduce_layers.so")
-LAYERS_SOURCES = ["layers.cpp", "norm_rows.hip", "norm_forward.hip", "norm_backward.hip", "dropout_kernels.hip", "loss_kernels.hip"]
+LAYERS_SOURCES = ["layers.cpp", "norm_rows.hip", "norm_forward.hip", "norm_backward.hip", "dropout_kernels.hip", "loss_kernels.hip",
+                  "embedding_kernels.hip", "log_probs_kernels.hip", "distill_kernels.hip"]
 # the packed-fp32 target feature is switched off for all device code
 DEVICE_FLAGS = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

@@ -129,6 +129,39 @@ int read_mask(const cr_dropout_t *d, cr::Mask *out)
     return CR_OK;
 }
 
+int check_rows(int64_t rows, int64_t classes, int dtype)
+{
+    if (rows < 0 || rows >= int64_t(1) << 31) return fail(CR_E_INVAL, "rows", " must be in 0 .. 2^31 - 1");
+    if (classes < 1 || classes > int64_t(1) << 28) return fail(CR_E_INVAL, "classes", " must be in 1 .. 2^28");
+    return dtype == CR_F32 || dtype == CR_BF16 ? CR_OK : fail(CR_E_INVAL, "dtype", " is unknown");
+}
+// rows x classes elements `row_stride` apart
+int read_rows(const void *p, int64_t row_stride, const cr::LayerShape &shape, bool output, const char *name)
+{
+    const cr_layer_view_t view = {const_cast<void *>(p), row_stride, 0};
+    cr::Rows unused;
+    return read_view(&view, shape, output, name, &unused);
+}
+int check_numbers(const void *p, bool required, const char *name)                 // of 64 bits
+{
+    if (!p) return required ? fail(CR_E_INVAL, name, " is required") : CR_OK;
+    return aligned(p, 8) ? CR_OK : fail(CR_E_INVAL, name, " is not 8-byte aligned");
+}
+
+int check_embedding(const cr::LayerShape &shape, int64_t vocabulary)
+{
+    if (shape.points * shape.positions >= int64_t(1) << 31) return fail(CR_E_INVAL, "points, positions", " must be less than 2^31 together");
+    return vocabulary >= 1 && vocabulary <= int64_t(1) << 28 ? CR_OK : fail(CR_E_INVAL, "vocabulary", " must be in 1 .. 2^28");
+}
+int read_tokens(const cr_layer_view_t *view, const cr::LayerShape &shape, cr::Rows *out)
+{
+    if (!view || !view->dev) return fail(CR_E_INVAL, "tokens", " is required");
+    if (!aligned(view->dev, 8)) return fail(CR_E_INVAL, "tokens", " is not 8-byte aligned");
+    cr::LayerShape one = shape;                          // strides as those of rows of one channel
+    one.channels = 1;
+    return read_view(view, one, false, "tokens", out);
+}
+
 }  // namespace
 
 extern "C" {
@@ -272,6 +305,137 @@ int cr_softmax_loss(int64_t rows, int64_t classes, int dtype, const void *logits
     CR_TRY(check_workspace(workspace, workspace_bytes, need));
     const cr::LossArgs a = {rows, static_cast<int>(classes), shape.bf16, logits, in.point_stride, targets, weights, loss, lse, dlogits, out.point_stride};
     return launched(cr::launch_loss(a, workspace, static_cast<hipStream_t>(hip_stream)), "cr_softmax_loss: ");
+}
+
+int cr_embedding_workspace_bytes(const cr_layer_shape_t *shape, int64_t vocabulary, const int64_t *bounds, int runs, size_t *backward_bytes)
+{
+    cr::LayerShape s;
+    int64_t whole[2];
+    const int64_t *b = nullptr;
+    CR_TRY(read_shape(shape, &s));
+    CR_TRY(check_embedding(s, vocabulary));
+    CR_TRY(read_bounds(s, bounds, runs, whole, &b));
+    if (!backward_bytes) return fail(CR_E_INVAL, "backward_bytes", " is required");
+    *backward_bytes = cr::embedding_backward_bytes(s, static_cast<int>(vocabulary), b, runs);
+    return CR_OK;
+}
+
+int cr_embedding_forward(const cr_layer_shape_t *shape, const cr_layer_view_t *tokens, const void *table, int table_dtype, int64_t vocabulary, float scale,
+                         const cr_layer_view_t *y, void *hip_stream)
+{
+    cr::EmbeddingArgs a = {};
+    CR_TRY(read_shape(shape, &a.shape));
+    CR_TRY(check_embedding(a.shape, vocabulary));
+    if (table_dtype != CR_F32 && table_dtype != CR_BF16) return fail(CR_E_INVAL, "table_dtype", " is unknown");
+    if (!std::isfinite(scale)) return fail(CR_E_INVAL, "scale", " must be finite");
+    if (a.shape.points == 0) return CR_OK;
+    CR_TRY(read_tokens(tokens, a.shape, &a.tokens));
+    if (!table || !aligned(table, table_dtype == CR_BF16 ? 2 : 4)) return fail(CR_E_INVAL, "table", " is required, aligned to its elements");
+    CR_TRY(read_view(y, a.shape, true, "y", &a.y));
+    a.table = table; a.table_bf16 = table_dtype == CR_BF16; a.vocabulary = static_cast<int>(vocabulary); a.scale = scale;
+    return launched(cr::launch_embedding_forward(a, static_cast<hipStream_t>(hip_stream)), "cr_embedding_forward: ");
+}
+
+int cr_embedding_backward(const cr_layer_shape_t *shape, const cr_layer_view_t *dy, const cr_layer_view_t *tokens, int64_t vocabulary, float scale,
+                          const int64_t *bounds, int runs, float *dtable, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    cr::EmbeddingGradArgs a = {};
+    int64_t whole[2];
+    CR_TRY(read_shape(shape, &a.shape));
+    CR_TRY(check_embedding(a.shape, vocabulary));
+    if (!std::isfinite(scale)) return fail(CR_E_INVAL, "scale", " must be finite");
+    CR_TRY(read_bounds(a.shape, bounds, runs, whole, &a.bounds));
+    CR_TRY(check_floats(dtable, true, "dtable"));
+    a.vocabulary = static_cast<int>(vocabulary); a.scale = scale; a.runs = runs; a.dtable = dtable;
+    if (a.shape.points > 0) {
+        CR_TRY(read_view(dy, a.shape, false, "dy", &a.dy));
+        CR_TRY(read_tokens(tokens, a.shape, &a.tokens));
+        CR_TRY(check_workspace(workspace, workspace_bytes, cr::embedding_backward_bytes(a.shape, a.vocabulary, a.bounds, runs)));
+    }
+    return launched(cr::launch_embedding_backward(a, workspace, static_cast<hipStream_t>(hip_stream)), "cr_embedding_backward: ");
+}
+
+int cr_log_probs_workspace_bytes(int64_t rows, int64_t classes, int dtype, int top, size_t *bytes)
+{
+    CR_TRY(check_rows(rows, classes, dtype));
+    if (top < 0 || top > 128) return fail(CR_E_INVAL, "top", " must be in 0 .. 128");
+    if (!bytes) return fail(CR_E_INVAL, "bytes", " is required");
+    *bytes = cr::log_probs_bytes(rows, classes, dtype == CR_BF16, top);
+    return CR_OK;
+}
+
+int cr_log_probs(int64_t rows, int64_t classes, int dtype, const void *logits, int64_t row_stride, const int64_t *tokens, float *logp, float *entropy, int top,
+                 int64_t *top_index, float *top_logp, float *largest, float *log_sum, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    size_t need = 0;
+    CR_TRY(cr_log_probs_workspace_bytes(rows, classes, dtype, top, &need));
+    if (rows == 0) return CR_OK;
+    const cr::LayerShape shape = {rows, 1, static_cast<int>(classes), dtype == CR_BF16};
+    CR_TRY(read_rows(logits, row_stride, shape, false, "logits"));
+    if (!tokens != !logp) return fail(CR_E_INVAL, "tokens, logp", " come together or not at all");
+    CR_TRY(check_numbers(tokens, false, "tokens"));
+    CR_TRY(check_floats(logp, false, "logp"));
+    CR_TRY(check_floats(entropy, false, "entropy"));
+    CR_TRY(check_numbers(top_index, top > 0, "top_index"));
+    CR_TRY(check_floats(top_logp, top > 0, "top_logp"));
+    if (!largest != !log_sum) return fail(CR_E_INVAL, "largest, log_sum", " come together or not at all");
+    CR_TRY(check_floats(largest, false, "largest"));
+    CR_TRY(check_floats(log_sum, false, "log_sum"));
+    CR_TRY(check_workspace(workspace, workspace_bytes, need));
+    const cr::LogProbsArgs a = {rows, shape.channels, shape.bf16, logits, rows > 1 ? row_stride : 0, tokens, logp, entropy, top, top_index, top_logp, largest, log_sum};
+    return launched(cr::launch_log_probs(a, workspace, static_cast<hipStream_t>(hip_stream)), "cr_log_probs: ");
+}
+
+int cr_log_probs_backward(int64_t rows, int64_t classes, int dtype, const void *logits, int64_t row_stride, const int64_t *tokens, const float *largest,
+                          const float *log_sum, const float *entropy, const float *dlogp, const float *dentropy, void *dlogits, int64_t dlogits_row_stride,
+                          void *hip_stream)
+{
+    CR_TRY(check_rows(rows, classes, dtype));
+    if (rows == 0) return CR_OK;
+    const cr::LayerShape shape = {rows, 1, static_cast<int>(classes), dtype == CR_BF16};
+    CR_TRY(read_rows(logits, row_stride, shape, false, "logits"));
+    CR_TRY(read_rows(dlogits, dlogits_row_stride, shape, true, "dlogits"));
+    if (!tokens != !dlogp) return fail(CR_E_INVAL, "tokens, dlogp", " come together or not at all");
+    if (!entropy != !dentropy) return fail(CR_E_INVAL, "entropy, dentropy", " come together or not at all");
+    CR_TRY(check_numbers(tokens, false, "tokens"));
+    CR_TRY(check_floats(largest, true, "largest"));
+    CR_TRY(check_floats(log_sum, true, "log_sum"));
+    CR_TRY(check_floats(entropy, false, "entropy"));
+    CR_TRY(check_floats(dlogp, false, "dlogp"));
+    CR_TRY(check_floats(dentropy, false, "dentropy"));
+    const cr::LogProbsGradArgs a = {rows, shape.channels, shape.bf16, logits, rows > 1 ? row_stride : 0, tokens, largest, log_sum, entropy, dlogp, dentropy, dlogits,
+                                    rows > 1 ? dlogits_row_stride : 0};
+    return launched(cr::launch_log_probs_backward(a, static_cast<hipStream_t>(hip_stream)), "cr_log_probs_backward: ");
+}
+
+int cr_distill_loss_workspace_bytes(int64_t rows, int64_t classes, int dtype, int top, size_t *bytes)
+{
+    CR_TRY(check_rows(rows, classes, dtype));
+    if (top < 1 || top > 128) return fail(CR_E_INVAL, "top", " must be in 1 .. 128");
+    if (!bytes) return fail(CR_E_INVAL, "bytes", " is required");
+    *bytes = cr::distill_bytes(rows, classes, dtype == CR_BF16, top);
+    return CR_OK;
+}
+
+int cr_distill_loss(int64_t rows, int64_t classes, int dtype, const void *logits, int64_t row_stride, int top, const int64_t *top_index,
+                    const float *top_logits, int64_t top_row_stride, float temperature, const float *weights, float *loss, void *dlogits,
+                    int64_t dlogits_row_stride, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    size_t need = 0;
+    CR_TRY(cr_distill_loss_workspace_bytes(rows, classes, dtype, top, &need));
+    if (!(temperature >= 0x1p-40f && temperature <= 0x1p40f)) return fail(CR_E_INVAL, "temperature", " must be in 2^-40 .. 2^40");
+    if (rows == 0) return CR_OK;
+    const cr::LayerShape shape = {rows, 1, static_cast<int>(classes), dtype == CR_BF16}, entries = {rows, 1, top, false};
+    CR_TRY(read_rows(logits, row_stride, shape, false, "logits"));
+    CR_TRY(check_numbers(top_index, true, "top_index"));
+    CR_TRY(read_rows(top_logits, top_row_stride, entries, false, "top_logits"));
+    CR_TRY(check_floats(weights, false, "weights"));
+    CR_TRY(check_floats(loss, true, "loss"));
+    if (dlogits) CR_TRY(read_rows(dlogits, dlogits_row_stride, shape, true, "dlogits"));
+    CR_TRY(check_workspace(workspace, workspace_bytes, need));
+    const cr::DistillArgs a = {rows, shape.channels, shape.bf16, logits, rows > 1 ? row_stride : 0, top, top_index, top_logits, rows > 1 ? top_row_stride : 0,
+                               temperature, weights, loss, dlogits, rows > 1 ? dlogits_row_stride : 0};
+    return launched(cr::launch_distill(a, workspace, static_cast<hipStream_t>(hip_stream)), "cr_distill_loss: ");
 }
 
 }  // extern "C"

@@ -83,4 +83,71 @@ struct LossArgs {
 size_t loss_bytes(int64_t rows, int64_t classes, bool bf16);
 hipError_t launch_loss(const LossArgs &a, void *workspace, hipStream_t stream);
 
+struct EmbeddingArgs {
+    LayerShape shape;
+    Rows tokens, y;
+    const void *table;
+    bool table_bf16;
+    int vocabulary;
+    float scale;
+};
+struct EmbeddingGradArgs {
+    LayerShape shape;
+    Rows dy, tokens;
+    int vocabulary;
+    float scale;
+    const int64_t *bounds;                               // host
+    int runs;
+    float *dtable;
+};
+size_t embedding_backward_bytes(const LayerShape &shape, int vocabulary, const int64_t *bounds, int runs);
+hipError_t launch_embedding_forward(const EmbeddingArgs &a, hipStream_t stream);
+hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace, hipStream_t stream);
+
+struct LogProbsArgs {
+    int64_t rows;
+    int classes;
+    bool bf16;
+    const void *logits;
+    int64_t row_stride;
+    const int64_t *tokens;                               // or null, with logp
+    float *logp, *entropy;                               // or null
+    int top;
+    int64_t *top_index;
+    float *top_logp, *largest, *log_sum;                 // the last two may be null
+};
+struct LogProbsGradArgs {
+    int64_t rows;
+    int classes;
+    bool bf16;
+    const void *logits;
+    int64_t row_stride;
+    const int64_t *tokens;                               // or null, with dlogp
+    const float *largest, *log_sum, *entropy, *dlogp, *dentropy;        // entropy and dentropy may be null
+    void *dlogits;
+    int64_t dlogits_row_stride;
+};
+size_t log_probs_bytes(int64_t rows, int64_t classes, bool bf16, int top);
+hipError_t launch_log_probs(const LogProbsArgs &a, void *workspace, hipStream_t stream);
+hipError_t launch_log_probs_backward(const LogProbsGradArgs &a, hipStream_t stream);
+
+struct DistillArgs {
+    int64_t rows;
+    int classes;
+    bool bf16;
+    const void *logits;
+    int64_t row_stride;
+    int top;
+    const int64_t *top_index;
+    const float *top_logits;
+    int64_t top_row_stride;
+    float temperature;
+    const float *weights;                                // or null
+    float *loss;
+    void *dlogits;                                       // or null
+    int64_t dlogits_row_stride;
+};
+size_t distill_bytes(int64_t rows, int64_t classes, bool bf16, int top);
+hipError_t launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream);
+
 }  // namespace cr

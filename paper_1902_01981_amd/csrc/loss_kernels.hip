@@ -12,49 +12,13 @@
 // and 913 us, 4.7 TB/s, of 131 071 classes, whose rows begin anywhere.  fp32, 4 099 x 50 008: 330 us, 5.0 TB/s.  Without it 32 768 x 4 096 bf16 43 us, 6.2 TB/s.
 // Narrow rows: 100 000 x 100 bf16 16 us, 2.5 TB/s.  3 x 131 072 fp32 13 us, the launches.  Rows wider than the registers: 8 192 x 152 064 bf16 1.55 ms, 4 096 x
 // 128 000 fp32 1.26 ms, both 5.0 TB/s of what moves, 3.3 of what has to.
-#include "layers_device.h"
+#include "softmax_device.h"
 
 #include <algorithm>
 
 namespace cr {
 
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-__device__ __forceinline__ float infinity() { return __builtin_inff(); }
-// e^v for v <= 0, the distance from the largest logit: off by |v| + 2 units of 2^-24 of itself, by less than 3 of them of the largest share, whose v is 0.
-// Results below 2^-126 are 0.
-__device__ __forceinline__ float exp_fast(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
-
-// c = reference, S = sum; c is finite unless the part has nothing but -infinity (S = 0 then) or a +infinity (S is NaN then)
-struct Softmax {
-    float c = -__builtin_inff(), S = 0.f;
-};
-// a reference that can be subtracted: 0 stands in where nothing has been seen but -infinity (or NaN, which the sum then shows)
-__device__ __forceinline__ float usable(float c) { return c == -infinity() ? 0.f : c; }
-
-// element offset of chunk q of a row: the last one is moved back to end with the row
-template <int VEC> __device__ __forceinline__ int chunk_at(int q, int nq, int classes) { return q < nq - 1 ? q * VEC : classes - VEC; }
-
-// Adds VEC elements, if they count.
-template <int VEC> __device__ __forceinline__ void take(Softmax &s, const float (&x)[VEC], bool count)
-{
-    float most = x[0];
-#pragma unroll
-    for (int v = 1; v < VEC; ++v) most = fmaxf(most, x[v]);
-    const float c = count ? fmaxf(s.c, most) : s.c, from = usable(c);
-    float sum = 0.f;
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) sum += exp_fast(x[v] - from);
-    s.S = s.S * exp_fast(s.c - from) + (count ? sum : 0.f);
-    s.c = c;
-}
-template <int LANES> __device__ __forceinline__ void join_lanes(Softmax &s)
-{
-    const float c = lanes_most<LANES>(s.c);
-    s.S = lanes_total<LANES>(s.S * exp_fast(s.c - usable(c)));
-    s.c = c;
-}
 
 // what the rows' outputs are made of
 struct RowTarget {

@@ -21,7 +21,9 @@ LAYERS_LIB_PATH = os.path.join(_HERE, "libcodedreduce_layers.so")
 CR_ACT_NONE, CR_ACT_RELU, CR_ACT_SILU = 0, 1, 2
 
 LAYERS_EXPORTS = ["cr_layers_last_error", "cr_group_norm_workspace_bytes", "cr_group_norm_forward", "cr_group_norm_backward",
-                  "cr_dropout_workspace_bytes", "cr_dropout_forward", "cr_dropout_backward", "cr_softmax_loss_workspace_bytes", "cr_softmax_loss"]
+                  "cr_dropout_workspace_bytes", "cr_dropout_forward", "cr_dropout_backward", "cr_softmax_loss_workspace_bytes", "cr_softmax_loss",
+                  "cr_embedding_workspace_bytes", "cr_embedding_forward", "cr_embedding_backward", "cr_log_probs_workspace_bytes", "cr_log_probs",
+                  "cr_log_probs_backward", "cr_distill_loss_workspace_bytes", "cr_distill_loss"]
 
 
 class cr_layer_shape_t(ctypes.Structure):
@@ -58,6 +60,15 @@ def load_layers_library():
         lib.cr_dropout_backward.argtypes = [shape, view, drop, view, vp, c_int, vp, vp, size_t, vp]
         lib.cr_softmax_loss_workspace_bytes.argtypes = [i64, i64, c_int, size_p]
         lib.cr_softmax_loss.argtypes = [i64, i64, c_int, vp, i64, vp, vp, vp, vp, vp, i64, vp, size_t, vp]
+        f32 = ctypes.c_float
+        lib.cr_embedding_workspace_bytes.argtypes = [shape, i64, vp, c_int, size_p]
+        lib.cr_embedding_forward.argtypes = [shape, view, vp, c_int, i64, f32, view, vp]
+        lib.cr_embedding_backward.argtypes = [shape, view, view, i64, f32, vp, c_int, vp, vp, size_t, vp]
+        lib.cr_log_probs_workspace_bytes.argtypes = [i64, i64, c_int, c_int, size_p]
+        lib.cr_log_probs.argtypes = [i64, i64, c_int, vp, i64, vp, vp, vp, c_int, vp, vp, vp, vp, vp, size_t, vp]
+        lib.cr_log_probs_backward.argtypes = [i64, i64, c_int, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, vp]
+        lib.cr_distill_loss_workspace_bytes.argtypes = [i64, i64, c_int, c_int, size_p]
+        lib.cr_distill_loss.argtypes = [i64, i64, c_int, vp, i64, c_int, vp, vp, i64, f32, vp, vp, vp, i64, vp, size_t, vp]
         _lib = lib
     return _lib
 
@@ -270,3 +281,111 @@ def cr_softmax_loss(logits, targets, loss, lse=None, dlogits=None, weights=None,
     _check(load_layers_library().cr_softmax_loss(rows, classes, shape.dtype, x.dev, x.point_stride, _vector(targets, rows, "targets", torch.int64, False),
                                                  _vector(weights, rows, "weights"), _vector(loss, rows, "loss", optional=False),
                                                  _vector(lse, rows, "lse"), dx.dev, dx.point_stride, ws, nbytes, _stream(stream)))
+
+
+# ---- token embedding -----------------------------------------------------------------------------------------------------
+def _tokens(t, like):
+    """The view of tokens, one for each position of `like`."""
+    _on_device(t, "tokens")
+    if t.dtype != torch.int64 or t.shape != like.shape[:-1]:
+        raise ValueError(f"tokens has shape {tuple(t.shape)} and dtype {t.dtype}, expected {tuple(like.shape[:-1])} and torch.int64")
+    return _view(t[..., None], t[..., None], "tokens")
+
+
+def cr_embedding_workspace_bytes(dy, vocabulary: int, bounds=None) -> int:
+    b = ctypes.c_size_t()
+    at, runs, _keep = _bounds(bounds)
+    _check(load_layers_library().cr_embedding_workspace_bytes(_shape_of(dy, "dy"), vocabulary, at, runs, ctypes.byref(b)))
+    return b.value
+
+
+def cr_embedding_forward(tokens, table, y, scale: float = 1.0, stream=None) -> None:
+    """tokens: int64 of the shape of y without its channels; table (vocabulary, channels), of a type of its own."""
+    shape, tables = _shape_of(y, "y"), _shape_of(table, "table")
+    if table.dim() != 2 or table.shape[1] != shape.channels or not table.is_contiguous():
+        raise ValueError(f"table must be contiguous and have the shape (vocabulary, {shape.channels})")
+    _check(load_layers_library().cr_embedding_forward(shape, _tokens(tokens, y), table.data_ptr(), tables.dtype, tables.points, scale, _view(y, y, "y"),
+                                                      _stream(stream)))
+
+
+def cr_embedding_backward(dy, tokens, dtable, scale: float = 1.0, bounds=None, workspace=None, stream=None) -> None:
+    """dtable: float32 (vocabulary, channels), or (runs, vocabulary, channels)."""
+    lib = load_layers_library()
+    shape = _shape_of(dy, "dy")
+    at, runs, _keep = _bounds(bounds)
+    if not isinstance(dtable, torch.Tensor) or dtable.dim() not in (2, 3) or dtable.shape[-1] != shape.channels or (dtable.shape[0] if dtable.dim() == 3 else 1) != runs:
+        raise ValueError(f"dtable must have the shape ({runs}, vocabulary, {shape.channels})")
+    vocabulary = dtable.shape[-2]
+    need = ctypes.c_size_t()
+    _check(lib.cr_embedding_workspace_bytes(shape, vocabulary, at, runs, ctypes.byref(need)))
+    ws, nbytes, _keep_ws = _workspace(workspace, need.value, stream)
+    _check(lib.cr_embedding_backward(shape, _view(dy, dy, "dy"), _tokens(tokens, dy), vocabulary, scale, at, runs,
+                                     _vector(dtable, runs * vocabulary * shape.channels, "dtable", optional=False), ws, nbytes, _stream(stream)))
+
+
+# ---- log probabilities ---------------------------------------------------------------------------------------------------
+def _rows_of(logits):
+    shape = _shape_of(logits, "logits")
+    if logits.dim() != 2:
+        raise ValueError("logits must have the shape (rows, classes)")
+    return shape
+
+
+def cr_log_probs_workspace_bytes(rows: int, classes: int, dtype: int, top: int = 0) -> int:
+    b = ctypes.c_size_t()
+    _check(load_layers_library().cr_log_probs_workspace_bytes(rows, classes, dtype, top, ctypes.byref(b)))
+    return b.value
+
+
+def cr_log_probs(logits, tokens=None, logp=None, entropy=None, top_index=None, top_logp=None, largest=None, log_sum=None, workspace=None, stream=None) -> None:
+    """logits (rows, classes); top_index, top_logp (rows, top)."""
+    shape = _rows_of(logits)
+    rows, top = shape.points, 0
+    if (top_index is None) != (top_logp is None):
+        raise ValueError("top_index and top_logp come together or not at all")
+    if top_index is not None:
+        if top_index.dim() != 2 or top_index.shape[0] != rows or top_index.shape != top_logp.shape:
+            raise ValueError("top_index and top_logp must have the shape (rows, top)")
+        top = top_index.shape[1]
+    x = _view(logits, logits, "logits")
+    ws, nbytes, _keep = _workspace(workspace, cr_log_probs_workspace_bytes(rows, shape.channels, shape.dtype, top), stream)
+    _check(load_layers_library().cr_log_probs(rows, shape.channels, shape.dtype, x.dev, x.point_stride, _vector(tokens, rows, "tokens", torch.int64),
+                                              _vector(logp, rows, "logp"), _vector(entropy, rows, "entropy"), top,
+                                              _vector(top_index, rows * top, "top_index", torch.int64), _vector(top_logp, rows * top, "top_logp"),
+                                              _vector(largest, rows, "largest"), _vector(log_sum, rows, "log_sum"), ws, nbytes, _stream(stream)))
+
+
+def cr_log_probs_backward(logits, tokens, largest, log_sum, entropy, dlogp, dentropy, dlogits, stream=None) -> None:
+    """dlogits may be logits itself; tokens and dlogp, or entropy and dentropy, may be None."""
+    shape = _rows_of(logits)
+    rows = shape.points
+    x, dx = _view(logits, logits, "logits"), _view(dlogits, logits, "dlogits")
+    _check(load_layers_library().cr_log_probs_backward(rows, shape.channels, shape.dtype, x.dev, x.point_stride, _vector(tokens, rows, "tokens", torch.int64),
+                                                       _vector(largest, rows, "largest", optional=False), _vector(log_sum, rows, "log_sum", optional=False),
+                                                       _vector(entropy, rows, "entropy"), _vector(dlogp, rows, "dlogp"), _vector(dentropy, rows, "dentropy"),
+                                                       dx.dev, dx.point_stride, _stream(stream)))
+
+
+# ---- distillation --------------------------------------------------------------------------------------------------------
+def cr_distill_loss_workspace_bytes(rows: int, classes: int, dtype: int, top: int) -> int:
+    b = ctypes.c_size_t()
+    _check(load_layers_library().cr_distill_loss_workspace_bytes(rows, classes, dtype, top, ctypes.byref(b)))
+    return b.value
+
+
+def cr_distill_loss(logits, top_index, top_logits, loss, temperature: float = 1.0, dlogits=None, weights=None, workspace=None, stream=None) -> None:
+    """logits (rows, classes); top_index int64 and top_logits float32, (rows, top), with the same distance from row to row; dlogits may be logits itself."""
+    shape = _rows_of(logits)
+    rows = shape.points
+    for t, name, dtype in ((top_index, "top_index", torch.int64), (top_logits, "top_logits", torch.float32)):
+        _on_device(t, name)
+        if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or (t.shape[1] > 1 and t.stride(1) != 1):
+            raise ValueError(f"{name} must be {dtype}, of the shape (rows, top), with the entries of a row side by side")
+    if top_index.shape != top_logits.shape or (rows > 1 and top_index.stride(0) != top_logits.stride(0)):
+        raise ValueError("top_index and top_logits must have the same shape and strides")
+    x = _view(logits, logits, "logits")
+    dx = cr_layer_view_t(0, 0, 0) if dlogits is None else _view(dlogits, logits, "dlogits")
+    ws, nbytes, _keep = _workspace(workspace, cr_distill_loss_workspace_bytes(rows, shape.channels, shape.dtype, top_index.shape[1]), stream)
+    _check(load_layers_library().cr_distill_loss(rows, shape.channels, shape.dtype, x.dev, x.point_stride, top_index.shape[1], top_index.data_ptr(),
+                                                 top_logits.data_ptr(), top_index.stride(0), temperature, _vector(weights, rows, "weights"),
+                                                 _vector(loss, rows, "loss", optional=False), dx.dev, dx.point_stride, ws, nbytes, _stream(stream)))

@@ -2,6 +2,11 @@
 //
 // With q the teacher's shares at temperature T, about their largest logit, and c, S as of the softmax loss with exp(x / T) in place of exp(x):
 //     loss = w T sum_i q_i ((z_i - largest z) - (x_(j_i) - c) + T (log S - log S_q)),   dx_j = w T (exp((x_j - c) / T) / S - sum_(j_i = j) q_i).
+//
+//   distill_wave_kernel    a row in the registers of a wavefront
+//   distill_rows_kernel    a row in the registers of a workgroup, read once; a wavefront of its own reads the teacher's entries, forms the loss and puts the
+//                          teacher's classes into the gradient
+//   distill_slices_kernel, distill_join_kernel   rows wider than that: a row cut into slices, read twice
 #include "softmax_device.h"
 
 #include <algorithm>
@@ -10,39 +15,53 @@ namespace cr {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64, kMostTop = 128, kEntries = kMostTop / 64;     // entries of a lane
+constexpr int kMostTop = 128, kEntries = kMostTop / 64;  // entries of a lane
 
 __device__ __forceinline__ float first_lane(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
 
 // What a wavefront knows of a row's teacher: entries lane and lane + 64.
 struct Teacher {
     int index[kEntries];         // -1: not there
     float q[kEntries];           // shares
     float d[kEntries];           // distances from the largest logit
+    float at[kEntries];          // the student's logits there
     bool any, unknown;           // entries at all; one of no class
     float sum;                   // of exp(d / T): NaN where there is no sense in it
+    float w;
 };
-__device__ __forceinline__ void read_teacher(Teacher &t, const DistillArgs &a, int64_t row, float unit)
+// A row's entries as they are given.
+struct Entries {
+    int64_t index[kEntries];
+    float z[kEntries], w;
+};
+__device__ __forceinline__ void read_entries(Entries &n, const DistillArgs &a, int64_t row)
 {
-    const int lane = threadIdx.x % 64;
-    float z[kEntries], most = -infinity();
-    bool there = false, unknown = false;
+    n.w = a.weights ? a.weights[row] : 1.f;
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) {
-        const int i = lane + 64 * e;
-        int64_t index = -1;
-        z[e] = -infinity();
+        const int i = threadIdx.x % 64 + 64 * e;
+        n.index[e] = -1;
+        n.z[e] = -infinity();
         if (i < a.top) {
-            index = a.top_index[row * a.top_row_stride + i];
-            z[e] = a.top_logits[row * a.top_row_stride + i];
+            n.index[e] = a.top_index[row * a.top_row_stride + i];
+            n.z[e] = a.top_logits[row * a.top_row_stride + i];
         }
-        if (index < 0 || z[e] == -infinity()) {
-            index = -1;
-            z[e] = -infinity();
-        }
-        there |= index >= 0;
-        unknown |= index >= a.classes;
-        t.index[e] = index >= a.classes ? -1 : static_cast<int>(index);
+    }
+}
+// All of it but the student's logits; their places.
+__device__ __forceinline__ void settle(Teacher &t, const Entries &n, const DistillArgs &a, float unit)
+{
+    float z[kEntries], most = -infinity();
+    bool there = false, unknown = false;
+    t.w = n.w;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        const bool is = n.index[e] >= 0 && n.z[e] != -infinity(), known = is && n.index[e] < a.classes;
+        z[e] = is ? n.z[e] : -infinity();
+        t.index[e] = known ? static_cast<int>(n.index[e]) : -1;
+        there |= is;
+        unknown |= is && !known;
         most = fmaxf(most, z[e]);
     }
     most = lanes_most<64>(most);
@@ -61,110 +80,530 @@ __device__ __forceinline__ void read_teacher(Teacher &t, const DistillArgs &a, i
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) t.q[e] *= by;
 }
+template <bool BF16> __device__ __forceinline__ void read_logits(float (&at)[kEntries], const Entries &n, const DistillArgs &a, int64_t row)
+{
+    const auto *x = static_cast<const typename Element<BF16>::type *>(a.logits) + row * a.row_stride;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) at[e] = Element<BF16>::get(x + (n.index[e] >= 0 && n.index[e] < a.classes ? n.index[e] : 0));
+}
+// what a row's gradient is, but for the shares
+enum Kind : int { kShares, kZero, kNan };
+__device__ __forceinline__ Kind kind_of(const Teacher &t) { return !t.any ? kZero : t.unknown || !(t.sum == t.sum) ? kNan : kShares; }
 
-template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) distill_kernel(DistillArgs a)
+// The loss, for every lane.
+__device__ __forceinline__ float loss_of(const Teacher &t, const DistillArgs &a, const Softmax &s)
+{
+    // Not distances over T, and a fourth of each: they, and sums of them, could be infinite where the loss is not (masks of the type's lowest value).
+    const float from = usable(s.c), both = 0.25f * a.temperature * kLn2 * (__builtin_amdgcn_logf(s.S) - __builtin_amdgcn_logf(t.sum));
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) {
+        const float term = t.q[e] * (0.25f * t.d[e] - (0.25f * t.at[e] - 0.25f * from) + both);
+        sum += t.index[e] >= 0 && t.q[e] != 0.f ? term : 0.f;
+    }
+    sum = lanes_total<64>(sum);
+    return !t.any ? 0.f : 4.f * (t.w * a.temperature * (t.unknown ? __builtin_nanf("") : s.S == 0.f ? infinity() * t.sum : sum));
+}
+// The gradient at the teacher's classes: an index that comes several times has the same bits from each of its entries.
+__device__ __forceinline__ void at_entries(float (&value)[kEntries], const Teacher &t, const DistillArgs &a, const Softmax &s, float unit, float factor)
+{
+    float q[kEntries];
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) q[e] = 0.f;
+#pragma unroll
+    for (int f = 0; f < kEntries; ++f) {
+        const int count = min(64, a.top - 64 * f);
+        for (int i = 0; i < count; ++i) {
+            const int index = __builtin_amdgcn_readlane(t.index[f], i);
+            const float share = lane_of(t.q[f], i);
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e) q[e] += t.index[e] == index ? share : 0.f;
+        }
+    }
+    const float from = usable(s.c);
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) value[e] = fmaf(exp_fast(t.at[e] - from, unit), factor, -(t.w * a.temperature * q[e]));
+}
+
+// ---- a wavefront's rows ----------------------------------------------------------------------------------------------------------
+// A lane has K chunks; the last chunk of a row is moved back to end with it, where it has elements twice: they count once and are stored twice, the same bits.
+template <bool BF16, int VEC, int K, bool GRAD> __global__ void __launch_bounds__(256) distill_wave_kernel(DistillArgs a)
 {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
-    __shared__ float meet[2][kWaves], shares[kMostTop];
-    __shared__ int places[kMostTop];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int whole = a.classes / VEC, left = a.classes % VEC;
+    const int lane = threadIdx.x % 64, nq = (a.classes + VEC - 1) / VEC, doubled = nq * VEC - a.classes;
     const float unit = kLog2e / a.temperature;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    for (int64_t row = int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); row < a.rows; row += int64_t(gridDim.x) * 4) {
         const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
-        Teacher teacher;
-        read_teacher(teacher, a, row, unit);
-        float at[kEntries];
+        typename C::raw raw[K];
 #pragma unroll
-        for (int e = 0; e < kEntries; ++e) at[e] = Element<BF16>::get(x + max(teacher.index[e], 0));
+        for (int k = 0; k < K; ++k) raw[k] = C::load(x + chunk_at<VEC>(min(lane + 64 * k, nq - 1), nq, a.classes));
+        Entries entries;
+        Teacher teacher;
+        read_entries(entries, a, row);
+        read_logits<BF16>(teacher.at, entries, a, row);
+        settle(teacher, entries, a, unit);
         Softmax s;
         float v[VEC];
-        for (int q = threadIdx.x; q < whole; q += kThreads) {
-            C::widen(C::load(x + q * VEC), v);
-            take<VEC>(s, v, true, unit);
-        }
-        if (threadIdx.x < left) {
-            const float last[1] = {Element<BF16>::get(x + whole * VEC + threadIdx.x)};
-            take<1>(s, last, true, unit);
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int q = lane + 64 * k;
+            C::widen(raw[k], v);
+            if (q == nq - 1) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = i < doubled ? -infinity() : v[i];
+            }
+            take<VEC>(s, v, q < nq, unit);
         }
         join_lanes<64>(s, unit);
-        __syncthreads();                                 // the last row's places are read
-        if (lane == 0) {
-            meet[0][wave] = s.c;
-            meet[1][wave] = s.S;
-        }
-        if (wave == 0) {
-#pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                places[lane + 64 * e] = teacher.index[e];
-                shares[lane + 64 * e] = teacher.q[e];
-            }
-        }
-        __syncthreads();
-        s.c = meet[0][threadIdx.x % kWaves];
-        s.S = meet[1][threadIdx.x % kWaves];
-        join_lanes<kWaves>(s, unit);
         s.c = first_lane(s.c);                           // the lanes' sums may differ by a rounding
         s.S = first_lane(s.S);
-        const float w = a.weights ? a.weights[row] : 1.f, from = usable(s.c), log2_S = __builtin_amdgcn_logf(s.S);
-        const float nan = __builtin_nanf("");
-        if (wave == 0) {
-            // Not distances over T, and a fourth of each: they, and sums of them, could be infinite where the loss is not (masks of the type's lowest value).
-            float sum = 0.f;
-            const float both = 0.25f * a.temperature * kLn2 * (log2_S - __builtin_amdgcn_logf(teacher.sum));
+        const float loss = loss_of(teacher, a, s);
+        if (lane == 0) a.loss[row] = loss;
+        if constexpr (GRAD) {
+            T *dx = static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride;
+            const Kind kind = kind_of(teacher);
+            const bool flat = kind != kShares || s.S == 0.f;
+            const float value = kind == kNan ? __builtin_nanf("") : 0.f, from = usable(s.c), factor = teacher.w * a.temperature / s.S;
 #pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                const float term = teacher.q[e] * (0.25f * teacher.d[e] - (0.25f * at[e] - 0.25f * from) + both);
-                sum += teacher.index[e] >= 0 && teacher.q[e] != 0.f ? term : 0.f;
+            for (int k = 0; k < K; ++k) {
+                const int q = lane + 64 * k;
+                if (q >= nq) break;
+                hold(raw[k]);                            // widened again rather than kept wide since the sum
+                C::widen(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = flat ? value : exp_fast(v[i] - from, unit) * factor;
+                C::store(dx + chunk_at<VEC>(q, nq, a.classes), C::narrow(v));
             }
-            sum = lanes_total<64>(sum);
-            if (lane == 0)
-                a.loss[row] = !teacher.any ? 0.f : 4.f * (w * a.temperature * (teacher.unknown ? nan : s.S == 0.f ? infinity() * teacher.sum : sum));
-        }
-        if (!a.dlogits) continue;
-        T *dx = static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride;
-        const bool no_sense = teacher.unknown || !(teacher.sum == teacher.sum);
-        const bool flat = !teacher.any || no_sense || s.S == 0.f;
-        const float value = teacher.any && no_sense ? nan : 0.f;
-        const float factor = w * a.temperature / s.S;
-        auto form = [&](float xi) { return flat ? value : exp_fast(xi - from, unit) * factor; };
-        for (int q = threadIdx.x; q < whole; q += kThreads) {
-            C::widen(C::load(x + q * VEC), v);
+            if (!flat) {
+                float put[kEntries];
+                at_entries(put, teacher, a, s, unit, factor);
+                // behind the shares of the same places
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = form(v[i]);
-            C::store(dx + q * VEC, C::narrow(v));
-        }
-        if (threadIdx.x < left) {
-            const int j = whole * VEC + threadIdx.x;
-            Element<BF16>::put(dx + j, form(Element<BF16>::get(x + j)));
-        }
-        __syncthreads();
-        // the teacher's classes follow; an index that comes several times has the same bits from each of its entries
-        if (wave == 0 && !flat) {
-#pragma unroll
-            for (int e = 0; e < kEntries; ++e) {
-                if (teacher.index[e] < 0) continue;
-                float q = 0.f;
-                for (int i = 0; i < a.top; ++i) q += places[i] == teacher.index[e] ? shares[i] : 0.f;
-                Element<BF16>::put(dx + teacher.index[e], fmaf(exp_fast(at[e] - from, unit), factor, -(w * a.temperature * q)));
+                for (int e = 0; e < kEntries; ++e)
+                    if (teacher.index[e] >= 0) Element<BF16>::put(dx + teacher.index[e], put[e]);
             }
         }
     }
 }
 
+// ---- a workgroup's rows ----------------------------------------------------------------------------------------------------------
+// All wavefronts but the last have chunks of the row, K a lane, lanes = ceil(whole / K) of them: as they were read, added to the running sum as they arrive, and
+// as soon as a chunk's gradient is stored its place takes the chunk of the workgroup's next row.  Whoever has no chunk at a place forms the last
+// whole one again, with the same bits, and does not count it.  The last wavefront has the elements behind the whole chunks, and the teacher: its entries' loads
+// depend on each other, and a wait for them would be a wait for all chunks in flight.  A row's barrier has the parts of its sums on one side and the
+// shares on the other; the teacher's classes follow behind the next one, when all shares have been stored.
+constexpr int kMostWaves = 16;
+template <bool BF16, int K, bool GRAD> __global__ void __launch_bounds__(64 * kMostWaves) distill_rows_kernel(DistillArgs a, int lanes)
+{
+    constexpr int VEC = BF16 ? 8 : 4;
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    constexpr unsigned kBytes = VEC * sizeof(T);
+    __shared__ float meet[2][2][kMostWaves];
+    __shared__ int kinds[2];
+    __shared__ float weights[2];
+    const int waves = blockDim.x / 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int whole = a.classes / VEC, left = a.classes % VEC;
+    const float unit = kLog2e / a.temperature;
+    int turn = 0;                                        // two places in turn: one barrier a row
+    auto meet_all = [&](Softmax &s) {
+        join_lanes<64>(s, unit);
+        if (threadIdx.x % 64 == 0) {
+            meet[turn][0][wave] = s.c;
+            meet[turn][1][wave] = s.S;
+        }
+        __syncthreads();
+        s = Softmax();
+        if (threadIdx.x % 16 < waves) {
+            s.c = meet[turn][0][threadIdx.x % 16];
+            s.S = meet[turn][1][threadIdx.x % 16];
+        }
+        join_lanes<16>(s, unit);
+        s.c = first_lane(s.c);                           // scalars, and the same for all: the lanes' sums may differ by a rounding
+        s.S = first_lane(s.S);
+    };
+    const int64_t stride = gridDim.x;
+    int64_t row = blockIdx.x;
+    if (row >= a.rows) return;                           // the whole workgroup
+
+    if (wave == waves - 1) {
+        const int lane = threadIdx.x % 64, edge_at = whole * VEC + min(lane, max(left - 1, 0));
+        const bool has_edge = lane < left;
+        int64_t last = -1;                               // the row before, whose classes are still to be put there
+        int places[kEntries];
+        float put[kEntries];
+        auto follow = [&] {
+            if (last < 0) return;
+            T *dx = static_cast<T *>(a.dlogits) + last * a.dlogits_row_stride;
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (places[e] >= 0) Element<BF16>::put(dx + places[e], put[e]);
+        };
+        // entries are read a row ahead, and the logits that they point at before this row's own work
+        Entries entries;
+        Teacher teacher;
+        float next_edge;
+        auto read_next = [&](int64_t of) {
+            read_logits<BF16>(teacher.at, entries, a, of);
+            next_edge = Element<BF16>::get(static_cast<const T *>(a.logits) + of * a.row_stride + min(edge_at, a.classes - 1));
+        };
+        read_entries(entries, a, row);
+        read_next(row);
+        for (; row < a.rows; row += stride) {
+            const int64_t next = std::min(row + stride, a.rows - 1);
+            settle(teacher, entries, a, unit);
+            const float edge = next_edge;
+            const float edges[1] = {edge};
+            read_entries(entries, a, next);
+            Softmax s;
+            take<1>(s, edges, has_edge, unit);
+            const Kind kind = kind_of(teacher);
+            if (lane == 0) {
+                kinds[turn] = kind;
+                weights[turn] = teacher.w;
+            }
+            meet_all(s);
+            turn ^= 1;
+            const Teacher now = teacher;
+            if (next != row) read_next(next);
+            const float loss = loss_of(now, a, s);
+            if (lane == 0) a.loss[row] = loss;
+            if constexpr (GRAD) {
+                follow();
+                const bool flat = kind != kShares || s.S == 0.f;
+                const float factor = now.w * a.temperature / s.S;
+                if (has_edge) {
+                    const float value = kind == kNan ? __builtin_nanf("") : 0.f;
+                    Element<BF16>::put(static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride + edge_at, flat ? value : exp_fast(edge - usable(s.c), unit) * factor);
+                }
+                last = flat ? -1 : row;
+                if (!flat) at_entries(put, now, a, s, unit, factor);
+#pragma unroll
+                for (int e = 0; e < kEntries; ++e) places[e] = now.index[e];
+            }
+        }
+        if constexpr (GRAD) {
+            __syncthreads();
+            follow();
+        }
+        return;
+    }
+
+    const int tl = min(static_cast<int>(threadIdx.x), lanes - 1);
+    auto row_at = [&](int64_t of) { return static_cast<const T *>(a.logits) + std::min(of, a.rows - 1) * a.row_stride; };
+    typename C::raw raw[K];
+    const unsigned lane_byte = tl * kBytes;
+    const unsigned last_byte = min(tl + (K - 1) * lanes, whole - 1) * kBytes;
+    auto chunk = [&](auto *x, int k) {                   // a scalar address and the lane's offset
+        using P = std::remove_pointer_t<decltype(x)>;
+        auto *bytes = reinterpret_cast<std::conditional_t<std::is_const_v<P>, const char, char> *>(x);
+        if (k < K - 1) return reinterpret_cast<P *>(scalar(bytes + static_cast<unsigned>(k * lanes) * kBytes) + lane_byte);
+        return reinterpret_cast<P *>(scalar(bytes) + last_byte);
+    };
+    auto fetch = [&](int k, const T *x) { raw[k] = GRAD ? C::load(chunk(x, k)) : C::load_once(chunk(x, k)); };
+    Softmax s;
+    auto add = [&](int k) {
+        float x[VEC];
+        C::widen(raw[k], x);
+        take<VEC>(s, x, k < K - 1 || static_cast<int>(threadIdx.x) + k * lanes < whole, unit);
+    };
+    auto settle = [&] {
+        if (static_cast<int>(threadIdx.x) >= lanes) s = Softmax();     // had the chunks of the last lane that has any
+    };
+    // the gradient of a row, each chunk making place for one of the row at x
+    auto form = [&](int64_t of, Kind kind, float w, auto more, const T *x) {
+        T *dx = static_cast<T *>(a.dlogits) + of * a.dlogits_row_stride;
+        const float from = usable(s.c), factor = w * a.temperature / s.S;
+        float v[VEC];
+        if (kind != kShares || s.S == 0.f) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = kind == kNan ? __builtin_nanf("") : 0.f;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                C::store(chunk(dx, k), C::narrow(v));
+                if (more()) fetch(k, x);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                hold(raw[k]);                            // widened again rather than kept wide since the sum
+                C::widen(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = exp_fast(v[i] - from, unit) * factor;
+                C::store(chunk(dx, k), C::narrow(v));
+                if (more()) fetch(k, x);
+            }
+        }
+    };
+
+    const T *x = row_at(row);
+#pragma unroll
+    for (int k = 0; k < K; ++k) fetch(k, x);
+    if constexpr (GRAD) {
+        auto step = [&](auto more) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) add(k);
+            settle();
+            meet_all(s);
+            const Kind kind = static_cast<Kind>(__builtin_amdgcn_readfirstlane(kinds[turn]));
+            const float w = first_lane(weights[turn]);
+            turn ^= 1;
+            form(row, kind, w, more, row_at(row + stride));
+            s = Softmax();
+        };
+        for (; row + stride < a.rows; row += stride) step(std::true_type());
+        step(std::false_type());
+        __syncthreads();
+    } else {
+        for (; row < a.rows; row += stride) {
+            x = row_at(row + stride);                    // past the last row: that row once more, from the caches
+            s = Softmax();
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                add(k);
+                fetch(k, x);
+            }
+            settle();
+            meet_all(s);
+            turn ^= 1;
+        }
+    }
+}
+
+// ---- a row in slices -------------------------------------------------------------------------------------------------------------
+constexpr int kSliceThreads = 256, kSliceChunks = 4;     // chunks that a thread has in flight
+__device__ __forceinline__ void join_block(Softmax &s, float (&lds)[2][kSliceThreads / 64], float unit)
+{
+    join_lanes<64>(s, unit);
+    if (threadIdx.x % 64 == 0) {
+        lds[0][threadIdx.x / 64] = s.c;
+        lds[1][threadIdx.x / 64] = s.S;
+    }
+    __syncthreads();
+    s.c = lds[0][threadIdx.x % (kSliceThreads / 64)];
+    s.S = lds[1][threadIdx.x % (kSliceThreads / 64)];
+    join_lanes<kSliceThreads / 64>(s, unit);
+    s.c = first_lane(s.c);
+    s.S = first_lane(s.S);
+}
+
+// parts[row of the batch][slice] = (c, S).  The logits at the teacher's classes go to at[row][entry]: in the next kernel the gradient may have replaced them.
+template <bool BF16, int VEC> __global__ void __launch_bounds__(kSliceThreads) distill_slices_kernel(DistillArgs a, int slice, f2 *parts, float *at)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    __shared__ float lds[2][kSliceThreads / 64];
+    const int nq = (a.classes + VEC - 1) / VEC, begin = blockIdx.x * slice, end = min(begin + slice, nq), doubled = nq * VEC - a.classes;
+    const int64_t row = blockIdx.y;
+    const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+    const float unit = kLog2e / a.temperature;
+    if (blockIdx.x == 0 && static_cast<int>(threadIdx.x) < a.top) {
+        const int64_t index = a.top_index[row * a.top_row_stride + threadIdx.x];
+        at[row * a.top + threadIdx.x] = Element<BF16>::get(x + (index >= 0 && index < a.classes ? index : 0));
+    }
+    Softmax s;
+    for (int q0 = begin + threadIdx.x; q0 < end; q0 += kSliceThreads * kSliceChunks) {
+        typename C::raw raw[kSliceChunks];
+#pragma unroll
+        for (int k = 0; k < kSliceChunks; ++k) raw[k] = C::load(x + chunk_at<VEC>(min(q0 + k * kSliceThreads, end - 1), nq, a.classes));
+#pragma unroll
+        for (int k = 0; k < kSliceChunks; ++k) {
+            const int q = q0 + k * kSliceThreads;
+            float v[VEC];
+            C::widen(raw[k], v);
+            if (q == nq - 1) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = i < doubled ? -infinity() : v[i];
+            }
+            take<VEC>(s, v, q < end, unit);
+        }
+    }
+    join_block(s, lds, unit);
+    if (threadIdx.x == 0) parts[row * gridDim.x + blockIdx.x] = f2{s.c, s.S};
+}
+// Joins a row's slices, every workgroup for itself, and forms the gradient of its own slice.
+template <bool BF16, int VEC, bool GRAD>
+__global__ void __launch_bounds__(kSliceThreads) distill_join_kernel(DistillArgs a, int slice, int slices, const f2 *parts, const float *at)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    __shared__ float lds[2][kSliceThreads / 64];
+    const int64_t row = blockIdx.y;
+    const int lane = threadIdx.x % 64;
+    const float unit = kLog2e / a.temperature;
+    Entries entries;
+    Teacher teacher;
+    read_entries(entries, a, row);
+    settle(teacher, entries, a, unit);
+#pragma unroll
+    for (int e = 0; e < kEntries; ++e) teacher.at[e] = at[row * a.top + min(lane + 64 * e, a.top - 1)];
+    Softmax s;
+    for (int i = threadIdx.x; i < slices; i += kSliceThreads) {
+        const f2 p = parts[row * slices + i];
+        const float c = fmaxf(s.c, p.x), from = usable(c);
+        s.S = s.S * exp_fast(s.c - from, unit) + p.y * exp_fast(p.x - from, unit);
+        s.c = c;
+    }
+    join_block(s, lds, unit);
+    if (blockIdx.x == 0 && threadIdx.x < 64) {
+        const float loss = loss_of(teacher, a, s);
+        if (lane == 0) a.loss[row] = loss;
+    }
+    if constexpr (GRAD) {
+        const int nq = (a.classes + VEC - 1) / VEC, begin = blockIdx.x * slice, end = min(begin + slice, nq);
+        const int doubled = nq * VEC - a.classes;
+        const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+        T *dx = static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride;
+        const Kind kind = kind_of(teacher);
+        const bool flat = kind != kShares || s.S == 0.f;
+        const float value = kind == kNan ? __builtin_nanf("") : 0.f, from = usable(s.c), factor = teacher.w * a.temperature / s.S;
+        for (int q0 = begin + threadIdx.x; q0 < end; q0 += kSliceThreads * kSliceChunks) {
+            typename C::raw raw[kSliceChunks];
+#pragma unroll
+            for (int k = 0; k < kSliceChunks; ++k) raw[k] = C::load(x + chunk_at<VEC>(min(q0 + k * kSliceThreads, end - 1), nq, a.classes));
+#pragma unroll
+            for (int k = 0; k < kSliceChunks; ++k) {
+                const int q = q0 + k * kSliceThreads, to = chunk_at<VEC>(q, nq, a.classes);
+                if (q >= end) break;
+                float v[VEC];
+                C::widen(raw[k], v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = flat ? value : exp_fast(v[i] - from, unit) * factor;
+                if (q < nq - 1 || doubled == 0) {
+                    C::store(dx + to, C::narrow(v));
+                } else {                                 // what the neighbour has too may have been read after it was replaced: it is the neighbour's
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i)
+                        if (i >= doubled) Element<BF16>::put(dx + to + i, v[i]);
+                }
+            }
+        }
+        if (flat) return;                                // the whole workgroup
+        __syncthreads();
+        if (threadIdx.x < 64) {                          // the teacher's classes in this slice follow
+            float put[kEntries];
+            at_entries(put, teacher, a, s, unit, factor);
+#pragma unroll
+            for (int e = 0; e < kEntries; ++e)
+                if (teacher.index[e] >= begin * VEC && teacher.index[e] < min(end * VEC, a.classes)) Element<BF16>::put(dx + teacher.index[e], put[e]);
+        }
+    }
+}
+
+struct DistillPlan {
+    int vec;
+    bool wave, slices;
+    int k, waves;                // chunks per lane, wavefronts of a workgroup with the teacher's
+    int slice, per_row;          // chunks of a slice, slices of a row
+    int64_t batch, with_gradient;        // rows per pair of launches: most; what the caches hold from its first to its second
+};
+constexpr int kFew = 8, kMany = 18;                      // chunks of a lane
+
+DistillPlan plan_distill(int64_t rows, int64_t classes, bool bf16)
+{
+    DistillPlan p = {};
+    p.vec = classes < (bf16 ? 8 : 4) ? 1 : bf16 ? 8 : 4;
+    const int64_t whole = classes / p.vec, chunks = (classes + p.vec - 1) / p.vec;
+    if (chunks <= 64 * 8) {
+        p.wave = true;
+        p.k = static_cast<int>((chunks + 63) / 64);
+        return p;
+    }
+    constexpr int kLanes = 64 * (kMostWaves - 1);
+    if (whole <= kLanes * kMany) {
+        p.k = whole <= kLanes * kFew ? kFew : kMany;
+        p.waves = 1 + static_cast<int>((whole + p.k * 64 - 1) / (p.k * 64));
+        return p;
+    }
+    constexpr int kStep = kSliceThreads * kSliceChunks;
+    p.slices = true;
+    int64_t slice = kStep;
+    while (whole > slice * 512) slice *= 2;
+    p.slice = static_cast<int>(slice);
+    p.per_row = static_cast<int>((chunks + slice - 1) / slice);
+    p.with_gradient = std::max<int64_t>(1, std::min<int64_t>(rows, (int64_t(64) << 20) / (classes * (bf16 ? 2 : 4))));
+    p.batch = std::max(p.with_gradient, std::min<int64_t>({rows, (int64_t(1) << 21) / p.per_row, 65535}));
+    return p;
+}
+
+constexpr int kUnits = 256;      // compute units, for the number of workgroups that stay
+
+template <bool BF16, int VEC, int K> void launch_wave(const DistillArgs &a, hipStream_t stream)
+{
+    const unsigned groups = static_cast<unsigned>(std::min<int64_t>((a.rows + 3) / 4, 1 << 20));
+    (a.dlogits ? distill_wave_kernel<BF16, VEC, K, true> : distill_wave_kernel<BF16, VEC, K, false>)<<<groups, 256, 0, stream>>>(a);
+}
+template <bool BF16, int K> void launch_rows(const DistillArgs &a, int waves, hipStream_t stream)
+{
+    // as many workgroups as the registers of the compute units take at once
+    constexpr int kWaves = K >= 16 ? 16 : 32;
+    const int lanes = (a.classes / (BF16 ? 8 : 4) + K - 1) / K;
+    const unsigned groups = static_cast<unsigned>(std::min<int64_t>(a.rows, kUnits * (kWaves / waves)));
+    (a.dlogits ? distill_rows_kernel<BF16, K, true> : distill_rows_kernel<BF16, K, false>)<<<groups, waves * 64, 0, stream>>>(a, lanes);
+}
+
+template <bool BF16> hipError_t launch(const DistillArgs &a, const DistillPlan &p, void *workspace, hipStream_t stream)
+{
+    constexpr int VEC = BF16 ? 8 : 4;
+    if (p.slices) {
+        f2 *parts = static_cast<f2 *>(workspace);
+        float *at = reinterpret_cast<float *>(parts + p.batch * p.per_row);
+        constexpr int64_t e = BF16 ? 2 : 4;
+        const int64_t batch = a.dlogits ? p.with_gradient : p.batch;
+        for (int64_t row = 0; row < a.rows; row += batch) {
+            DistillArgs b = a;
+            b.rows = std::min(batch, a.rows - row);
+            b.logits = static_cast<const char *>(a.logits) + row * a.row_stride * e;
+            b.top_index += row * a.top_row_stride;
+            b.top_logits += row * a.top_row_stride;
+            if (b.weights) b.weights += row;
+            b.loss += row;
+            if (b.dlogits) b.dlogits = static_cast<char *>(a.dlogits) + row * a.dlogits_row_stride * e;
+            const dim3 grid(p.per_row, static_cast<unsigned>(b.rows));
+            distill_slices_kernel<BF16, VEC><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, parts, at);
+            if (b.dlogits) distill_join_kernel<BF16, VEC, true><<<grid, kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts, at);
+            else distill_join_kernel<BF16, VEC, false><<<dim3(1, grid.y), kSliceThreads, 0, stream>>>(b, p.slice, p.per_row, parts, at);
+        }
+        return hipGetLastError();
+    }
+    if (p.vec == 1) {
+        launch_wave<BF16, 1, 1>(a, stream);
+    } else if (p.wave) {
+        switch (p.k) {
+        case 1: launch_wave<BF16, VEC, 1>(a, stream); break;
+        case 2: launch_wave<BF16, VEC, 2>(a, stream); break;
+        case 3: launch_wave<BF16, VEC, 3>(a, stream); break;
+        case 4: launch_wave<BF16, VEC, 4>(a, stream); break;
+        case 5: launch_wave<BF16, VEC, 5>(a, stream); break;
+        case 6: launch_wave<BF16, VEC, 6>(a, stream); break;
+        case 7: launch_wave<BF16, VEC, 7>(a, stream); break;
+        default: launch_wave<BF16, VEC, 8>(a, stream);
+        }
+    } else if (p.k == kFew) {
+        launch_rows<BF16, kFew>(a, p.waves, stream);
+    } else {
+        launch_rows<BF16, kMany>(a, p.waves, stream);
+    }
+    return hipGetLastError();
+}
+
 }  // namespace
 
-size_t distill_bytes(int64_t, int64_t, bool, int) { return 0; }
+size_t distill_bytes(int64_t rows, int64_t classes, bool bf16, int top)
+{
+    if (rows == 0) return 0;
+    const DistillPlan p = plan_distill(rows, classes, bf16);
+    return p.slices ? static_cast<size_t>(p.batch) * (p.per_row * sizeof(f2) + top * sizeof(float)) : 0;
+}
 
-hipError_t launch_distill(const DistillArgs &a, void *, hipStream_t stream)
+hipError_t launch_distill(const DistillArgs &a, void *workspace, hipStream_t stream)
 {
     if (a.rows == 0) return hipSuccess;
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>(a.rows, 1 << 20));
-    if (a.classes < (a.bf16 ? 8 : 4)) (a.bf16 ? distill_kernel<true, 1> : distill_kernel<false, 1>)<<<grid, kThreads, 0, stream>>>(a);
-    else if (a.bf16) distill_kernel<true, 8><<<grid, kThreads, 0, stream>>>(a);
-    else distill_kernel<false, 4><<<grid, kThreads, 0, stream>>>(a);
-    return hipGetLastError();
+    const DistillPlan p = plan_distill(a.rows, a.classes, a.bf16);
+    return a.bf16 ? launch<true>(a, p, workspace, stream) : launch<false>(a, p, workspace, stream);
 }
 
 }  // namespace cr

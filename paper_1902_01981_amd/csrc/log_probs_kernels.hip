@@ -113,75 +113,210 @@ template <bool WAVE> struct Team {
     }
 };
 
-// The largest number of 16 bits that at least `top` of a wavefront's numbers reach, 0 if there are no so many above 0.
+// The top-th largest of a wavefront's numbers of 16 bits, 0 if there are no so many above 0: bit by bit, from the first in which any differ.
 template <int N> __device__ __forceinline__ uint32_t reached(const uint32_t (&keys)[N], int top)
 {
-    uint32_t least = 0;
+    uint32_t all = keys[0], any = keys[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) {
+        all &= keys[i];
+        any |= keys[i];
+    }
+    // what the lanes have in common, as numbers of 16 bits beside each other
+    uint32_t both = any << 16 | (~all & 0xffffu);
+    both |= __builtin_amdgcn_update_dpp(0, both, 0xB1, 0xf, 0xf, false);
+    both |= __builtin_amdgcn_update_dpp(0, both, 0x4E, 0xf, 0xf, false);
+    both |= __builtin_amdgcn_update_dpp(0, both, 0x141, 0xf, 0xf, false);
+    both |= __builtin_amdgcn_update_dpp(0, both, 0x140, 0xf, 0xf, false);
+    const uint32_t joined = __builtin_amdgcn_readlane(both, 0) | __builtin_amdgcn_readlane(both, 16) | __builtin_amdgcn_readlane(both, 32) | __builtin_amdgcn_readlane(both, 48);
+    const uint32_t differ = joined >> 16 & joined & 0xffffu;         // bits that some have and some have not
+    const int first = 31 - __builtin_clz(differ | 1u);
+    uint32_t least = (joined >> 16 & ~differ) >> (first + 1) << (first + 1);
+    int reach = 0;
 #pragma unroll 1
-    for (int bit = 15; bit >= 0; --bit) {
+    for (int bit = first; bit >= 0; --bit) {
         const uint32_t more = least | 1u << bit;
         int count = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) count += __popcll(__ballot(keys[i] >= more));
-        if (count >= top) least = more;
+        if (count >= top) {
+            least = more;
+            reach = count;
+        }
     }
-    return least;
+    // no bit was taken: whether the prefix itself is reached is not known yet
+    if (reach == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) reach += __popcll(__ballot(keys[i] >= max(least, 1u)));
+    }
+    return reach >= top ? least : 0u;
 }
 __device__ __forceinline__ uint32_t short_key(float x) { return x > -infinity() ? ordered(x) >> 16 : 0u; }       // 0 of -infinity and NaN
 
 constexpr int kWaveEntries = 512, kBlockEntries = 1024;  // that a team keeps of those that may be among the largest
 
-template <bool BF16, int VEC, int K, bool WAVE>
-__global__ void __launch_bounds__(kThreads) log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint64_t *lists)
+// The `top` largest of chunks [begin, end) of a row, where too many are no smaller than `least`, equal ones mostly: the top-th largest value itself, which is the
+// smallest of them if all the others are too few, and is found bit by bit if not; then as many of its places as are wanted, lowest first.  The chunks are
+// read again each time: 32 KB at most, from the caches.
+template <bool BF16, int VEC, bool WAVE>
+__device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::element *x, int begin, int end, int nq, int classes, int top, float least, uint64_t *list, int *count, float *meet)
+{
+    using C = Chunk<BF16, VEC>;
+    using Group = Team<WAVE>;
+    const int lane = threadIdx.x % Group::kSize, doubled = nq * VEC - classes;
+    // f(number in order, index, value) for the elements of a step that are this thread's; places of a step lie behind those of the one before
+    auto of_step = [&](int q0, auto &&f) {
+        const int q = q0 + lane;
+        if (q >= end) return;
+        const int at = chunk_at<VEC>(q, nq, classes);
+        float v[VEC];
+        C::widen(C::load(x + at), v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i)
+            if (v[i] > -infinity() && (q < nq - 1 || i >= doubled)) f(ordered(v[i]), at + i, v[i]);
+    };
+    auto number = [&](auto &&counts) {
+        int mine = 0;
+        for (int q0 = begin; q0 < end; q0 += Group::kSize) of_step(q0, [&](uint32_t o, int, float) { mine += counts(o); });
+        return Group::total(mine, meet);
+    };
+    Group::sync();
+    float smallest = infinity();
+    for (int q0 = begin; q0 < end; q0 += Group::kSize) of_step(q0, [&](uint32_t, int, float v) { smallest = v >= least ? fminf(smallest, v) : smallest; });
+    smallest = -lanes_most<64>(-smallest);
+    if constexpr (!WAVE) {
+        if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = smallest;
+        __syncthreads();
+        smallest = fminf(fminf(meet[0], meet[1]), fminf(meet[2], meet[3]));
+        __syncthreads();
+    }
+    uint32_t value = ordered(smallest);
+    if (number([&](uint32_t o) { return o > value; }) >= top) {
+        value = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t more = value | 1u << bit;
+            if (number([&](uint32_t o) { return o >= more; }) >= top) value = more;
+        }
+    }
+    if (lane == 0) *count = 0;
+    Group::sync();
+    for (int q0 = begin; q0 < end; q0 += Group::kSize)
+        of_step(q0, [&](uint32_t o, int index, float v) {
+            if (o > value) {
+                const int to = atomicAdd(count, 1);
+                if (to < kMostTop) list[to] = entry_of(v, index);
+            }
+        });
+    Group::sync();
+    int n = min(*count, top);                            // fewer than `top`; places of the value itself fill them up
+    for (int q0 = begin; q0 < end && n < top; q0 += Group::kSize) {
+        int mine = 0;
+        of_step(q0, [&](uint32_t o, int, float) { mine += o == value; });
+        int sum = mine;                                  // up to and with this lane
+        for (int d = 1; d < 64; d *= 2) {
+            const int other = __shfl_up(sum, d);
+            if (static_cast<int>(threadIdx.x % 64) >= d) sum += other;
+        }
+        int total = __shfl(sum, 63), before = 0;
+        if constexpr (!WAVE) {
+            if (threadIdx.x % 64 == 63) meet[threadIdx.x / 64] = static_cast<float>(sum);
+            __syncthreads();
+            total = 0;
+            for (int w = 0; w < 4; ++w) {
+                if (w < static_cast<int>(threadIdx.x / 64)) before += static_cast<int>(meet[w]);
+                total += static_cast<int>(meet[w]);
+            }
+            __syncthreads();
+        }
+        int to = n + before + sum - mine;
+        of_step(q0, [&](uint32_t o, int index, float v) {
+            if (o == value) {
+                if (to < top) list[to] = entry_of(v, index);
+                ++to;
+            }
+        });
+        n = min(n + total, top);
+    }
+    Group::sync();
+    return n;
+}
+
+// K chunks of a lane; TOP: alternatives are wanted.  A team has one unit, a row or a slice of one: where it stayed and read the next unit's chunks as it was done with
+// these, 4 099 x 50 008 bf16 took 102 us and 246 with 64 alternatives, since that took registers from the other teams, whose loads hide the waits as well.
+// Arithmetic bounds it as much as reads do (an exponential is four operations), so a sweep over a lane's chunks has no operation too many: the largest first, then
+// the sums, E without a bound on the distances: where a class cannot be it is NaN (0 times infinity), and those lanes add up once more.
+constexpr int kWavesOf[2] = {6, 8};                      // of a SIMD: where a lane has eight chunks, and where it has fewer
+template <bool BF16, int VEC, int K, bool WAVE, bool TOP>
+__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesOf[K < 8])))
+log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint64_t *lists)
 {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
     using Group = Team<WAVE>;
-    constexpr int kTeams = kThreads / Group::kSize, kEntries = WAVE ? kWaveEntries : kBlockEntries;
+    constexpr int kTeams = kThreads / Group::kSize, kEntries = !TOP ? 1 : WAVE ? kWaveEntries : kBlockEntries;
     __shared__ uint64_t entries[kTeams][kEntries];
     __shared__ int counts[kTeams];
     __shared__ float meet[3][4];
-    __shared__ uint32_t maxima[WAVE ? 1 : kThreads];
+    __shared__ uint32_t maxima[WAVE || !TOP ? 1 : kThreads];
     __shared__ float bound;
     const int wave = threadIdx.x / 64, team = WAVE ? wave : 0, lane = threadIdx.x % Group::kSize;
-    const int64_t unit = WAVE ? int64_t(blockIdx.x) * kTeams + team : int64_t(blockIdx.x);
-    const int64_t row = WAVE ? unit : unit / slices;
+    const int unit = WAVE ? blockIdx.x * kTeams + team : blockIdx.x;               // fewer than 2^22 in a batch
+    const int row = WAVE || slices == 1 ? unit : unit / slices;
     if (row >= a.rows) return;                           // whole teams; there is no barrier of the workgroup where a team is a wavefront
-    const int nq = (a.classes + VEC - 1) / VEC, begin = WAVE ? 0 : static_cast<int>(unit - row * slices) * slice, end = min(begin + slice, nq);
+    const int nq = (a.classes + VEC - 1) / VEC, begin = WAVE ? 0 : (unit - row * slices) * slice, end = min(begin + slice, nq);
     const int doubled = nq * VEC - a.classes;            // of the last chunk, which is moved back to end with the row
     const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+    auto place = [&](int k) { return chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes); };
+    auto has = [&](int k) { return begin + lane + k * Group::kSize < end; };
 
     typename C::raw raw[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) raw[k] = C::load(x + chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes));
-    float v[VEC], most[K], c = -infinity();
+    for (int k = 0; k < K; ++k) raw[k] = C::load_once(x + place(k));
+    float v[VEC], most[K], own = -infinity();            // own: the largest of this thread
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        // what is no element of this place is a class that cannot be
-        const int q = begin + lane + k * Group::kSize, none = q >= end ? VEC : q == nq - 1 ? doubled : 0;
-        if (none) {
+        // what the neighbour has is here a class that cannot be
+        if (begin + lane + k * Group::kSize == nq - 1 && doubled > 0) {
             C::widen(raw[k], v);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = i < none ? -infinity() : v[i];
+            for (int i = 0; i < VEC; ++i) v[i] = i < doubled ? -infinity() : v[i];
             raw[k] = C::narrow(v);
         }
         C::widen(raw[k], v);
-        most[k] = v[0];
+        float m = v[0];
 #pragma unroll
-        for (int i = 1; i < VEC; ++i) most[k] = fmaxf(most[k], v[i]);
-        c = fmaxf(c, most[k]);
+        for (int i = 1; i < VEC; ++i) m = fmaxf(m, v[i]);
+        most[k] = has(k) ? m : -infinity();
+        own = fmaxf(own, most[k]);
+        hold(raw[k]);                                    // widened again later, rather than kept wide
     }
-    const float own = c;                                 // the largest of this thread
     Part p = {own, 0.f, 0.f, 0.f};
     const float from = usable(own);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        C::widen(raw[k], v);
+        if (has(k)) {
+            C::widen(raw[k], v);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float d = v[i] - from, e = exp_fast(d);
-            p.S += e;
-            p.E = fmaf(e, bounded(d), p.E);
+            for (int i = 0; i < VEC; ++i) {
+                const float d = v[i] - from, e = exp_fast(d);
+                p.S += e;
+                p.E = fmaf(e, d, p.E);
+            }
+        }
+        hold(raw[k]);
+    }
+    if (!(p.E == p.E)) {
+        p.E = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            if (!has(k)) continue;
+            C::widen(raw[k], v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float d = v[i] - from;
+                p.E = fmaf(exp_fast(d), bounded(d), p.E);
+            }
+            if constexpr (TOP) hold(raw[k]);
         }
     }
     join_lanes<64>(p);
@@ -191,147 +326,133 @@ __global__ void __launch_bounds__(kThreads) log_probs_slices_kernel(LogProbsArgs
             meet[1][wave] = p.S;
             meet[2][wave] = p.E;
         }
+        if constexpr (TOP) maxima[threadIdx.x] = short_key(own);
         __syncthreads();
         p = {meet[0][threadIdx.x % 4], meet[1][threadIdx.x % 4], meet[2][threadIdx.x % 4], 0.f};
         join_lanes<4>(p);
     }
-    const float log2_S = __builtin_amdgcn_logf(p.S);                 // the hardware's logarithm is that to base 2
+    const float log2_S = __builtin_amdgcn_logf(p.S);     // the hardware's logarithm is that to base 2
     const bool alone = WAVE || slices == 1;
     if (lane == 0) {
         if (alone) write_row(a, row, p, log2_S);
         else parts[unit] = p;
     }
-    if (a.top == 0) return;
-
-    float least;
-    if constexpr (WAVE) {
-        uint32_t keys[K];
+    if constexpr (TOP) {
+        uint64_t *list = entries[team];
+        int *count = &counts[team];
+        float least;
+        if constexpr (WAVE) {
+            // sets of a lane's elements: the chunks; where they are too few for a bound that is one, eight sets of a lane if it has so many elements
+            constexpr int kSets = K >= 8 || VEC == 1 ? 1 : VEC < 8 / K ? VEC : 8 / K, kOfSet = VEC / kSets;
+            uint32_t key;
+            if (kSets == 1 || 2 * a.top <= nq) {
+                uint32_t keys[K];
 #pragma unroll
-        for (int k = 0; k < K; ++k) keys[k] = short_key(most[k]);
-        const uint32_t key = reached(keys, a.top);
-        least = key ? unordered(key << 16) : kLowest;
-    } else {
-        maxima[threadIdx.x] = short_key(own);
-        __syncthreads();
-        if (wave == 0) {
+                for (int k = 0; k < K; ++k) keys[k] = short_key(most[k]);
+                key = reached(keys, a.top);
+            } else {
+                uint32_t keys[K * kSets];
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    C::widen(raw[k], v);
+#pragma unroll
+                    for (int set = 0; set < kSets; ++set) {
+                        float m = v[set * kOfSet];
+#pragma unroll
+                        for (int i = 1; i < kOfSet; ++i) m = fmaxf(m, v[set * kOfSet + i]);
+                        keys[k * kSets + set] = has(k) ? short_key(m) : 0u;
+                    }
+                }
+                key = reached(keys, a.top);
+            }
+            least = key ? unordered(key << 16) : kLowest;
+        } else if (wave == 0) {
             uint32_t keys[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) keys[i] = maxima[threadIdx.x + 64 * i];
             const uint32_t key = reached(keys, a.top);
             if (threadIdx.x == 0) bound = key ? unordered(key << 16) : kLowest;
         }
-    }
-    uint64_t *list = entries[team];
-    int *count = &counts[team];
-    if (lane == 0) *count = 0;
-    Group::sync();
-    if constexpr (!WAVE) least = bound;
-    if (own >= least) {
+        if (lane == 0) *count = 0;
+        Group::sync();
+        if constexpr (!WAVE) least = bound;
+        // the chunks with such elements, one of each lane at a time: few lanes have any, and fewer have several
+        unsigned chunks = 0;
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            if (most[k] < least) continue;
-            C::widen(raw[k], v);
-            const int at = chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes);
+        for (int k = 0; k < K; ++k) chunks |= most[k] >= least ? 1u << k : 0u;
+        while (chunks) {
+            const int which = __builtin_ctz(chunks);
+            chunks &= chunks - 1;
+            typename C::raw one = raw[0];
+#pragma unroll
+            for (int k = 1; k < K; ++k) one = which == k ? raw[k] : one;
+            C::widen(one, v);
+            const int at = chunk_at<VEC>(begin + lane + which * Group::kSize, nq, a.classes);
+            int hits = 0;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) hits += v[i] >= least;
+            int to = atomicAdd(count, hits);
 #pragma unroll
             for (int i = 0; i < VEC; ++i)
                 if (v[i] >= least) {
-                    const int to = atomicAdd(count, 1);
                     if (to < kEntries) list[to] = entry_of(v[i], at + i);
+                    ++to;
                 }
         }
-    }
-    Group::sync();
-    int n = *count;
-    if (n > kEntries) {
-        // Too many, equal ones mostly: the top-th largest value itself, bit by bit, then as many of its places as are wanted, lowest first.
-        auto number = [&](auto &&counts_if) {
-            int mine = 0;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                C::widen(raw[k], v);
-                const int at = chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) mine += v[i] > -infinity() && counts_if(ordered(v[i]), at + i);
-            }
-            return Group::total(mine, meet[0]);
+        Group::sync();
+        int n = *count;
+        if (n > kEntries) n = select_exactly<BF16, VEC, WAVE>(x, begin, end, nq, a.classes, a.top, least, list, count, meet[0]);
+        auto leave = [&](int rank, uint64_t entry) {
+            if (alone) write_entry(a, row, rank, entry, p, log2_S);
+            else lists[int64_t(unit) * a.top + rank] = entry;
         };
-        Group::sync();
-        uint32_t value = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t more = value | 1u << bit;
-            if (number([&](uint32_t o, int) { return o >= more; }) >= a.top) value = more;
+        for (int i = lane; i < n; i += Group::kSize) {
+            const uint64_t entry = list[i];
+            int rank = 0;
+#pragma unroll 8
+            for (int j = 0; j < n; ++j) rank += list[j] > entry;
+            if (rank < a.top) leave(rank, entry);
         }
-        const int wanted = a.top - number([&](uint32_t o, int) { return o > value; });
-        int behind = 0;                                  // the largest index before which there are fewer places than wanted
-        for (int bit = 28; bit >= 0; --bit) {
-            const int more = behind | 1 << bit;
-            if (more <= a.classes && number([&](uint32_t o, int index) { return o == value && index < more; }) < wanted) behind = more;
-        }
-        if (lane == 0) *count = 0;
-        Group::sync();
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            C::widen(raw[k], v);
-            const int at = chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const uint32_t o = ordered(v[i]);
-                if (v[i] > -infinity() && (o > value || (o == value && at + i <= behind))) {
-                    const int to = atomicAdd(count, 1);
-                    if (to < kEntries) list[to] = entry_of(v[i], at + i);
-                }
-            }
-        }
-        Group::sync();
-        n = min(*count, kEntries);
+        for (int rank = n + lane; rank < a.top; rank += Group::kSize) leave(rank, 0);
     }
-    auto leave = [&](int place, uint64_t entry) {
-        if (alone) write_entry(a, row, place, entry, p, log2_S);
-        else lists[unit * a.top + place] = entry;
-    };
-    for (int i = lane; i < n; i += Group::kSize) {
-        const uint64_t entry = list[i];
-        int place = 0;
-        for (int j = 0; j < n; ++j) place += list[j] > entry;
-        if (place < a.top) leave(place, entry);
-    }
-    for (int place = n + lane; place < a.top; place += Group::kSize) leave(place, 0);
 }
 
 // A row's slices: their sums, and the largest of their lists, a few lists at a time beside those found so far.  A number's place is the number of larger ones in
 // every list, each of which is in order.
 constexpr int kListsAtOnce = 8;
-__global__ void __launch_bounds__(kThreads) log_probs_join_kernel(LogProbsArgs a, int slices, const Part *parts, const uint64_t *lists)
+template <int THREADS> __global__ void __launch_bounds__(THREADS) log_probs_join_kernel(LogProbsArgs a, int slices, const Part *parts, const uint64_t *lists)
 {
     __shared__ uint64_t some[kListsAtOnce + 1][kMostTop], best[kMostTop];
     __shared__ float meet[3][4];
     const int64_t row = blockIdx.x;
     Part p = {-infinity(), 0.f, 0.f, 0.f};
-    for (int i = threadIdx.x; i < slices; i += kThreads) p = joined(p, parts[row * slices + i]);
+    for (int i = threadIdx.x; i < slices; i += THREADS) p = joined(p, parts[row * slices + i]);
     join_lanes<64>(p);
-    if (threadIdx.x % 64 == 0) {
-        meet[0][threadIdx.x / 64] = p.c;
-        meet[1][threadIdx.x / 64] = p.S;
-        meet[2][threadIdx.x / 64] = p.E;
+    if constexpr (THREADS > 64) {
+        if (threadIdx.x % 64 == 0) {
+            meet[0][threadIdx.x / 64] = p.c;
+            meet[1][threadIdx.x / 64] = p.S;
+            meet[2][threadIdx.x / 64] = p.E;
+        }
+        __syncthreads();
+        p = {meet[0][threadIdx.x % 4], meet[1][threadIdx.x % 4], meet[2][threadIdx.x % 4], 0.f};
+        join_lanes<4>(p);
     }
-    __syncthreads();
-    p = {meet[0][threadIdx.x % 4], meet[1][threadIdx.x % 4], meet[2][threadIdx.x % 4], 0.f};
-    join_lanes<4>(p);
     const float log2_S = __builtin_amdgcn_logf(p.S);                 // the hardware's logarithm is that to base 2
     if (threadIdx.x == 0) write_row(a, row, p, log2_S);
     const int top = a.top;
     if (top == 0) return;
-    if (threadIdx.x < top) best[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < top; i += THREADS) best[i] = 0;
     for (int first = 0; first < slices; first += kListsAtOnce) {
         const int now = min(kListsAtOnce, slices - first);
         __syncthreads();
-        for (int i = threadIdx.x; i < now * top; i += kThreads) some[1 + i / top][i % top] = lists[(row * slices + first) * top + i];
-        if (threadIdx.x < top) {
-            some[0][threadIdx.x] = best[threadIdx.x];
-            best[threadIdx.x] = 0;
+        for (int i = threadIdx.x; i < now * top; i += THREADS) some[1 + i / top][i % top] = lists[(row * slices + first) * top + i];
+        for (int i = threadIdx.x; i < top; i += THREADS) {
+            some[0][i] = best[i];
+            best[i] = 0;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < (now + 1) * top; i += kThreads) {
+        for (int i = threadIdx.x; i < (now + 1) * top; i += THREADS) {
             const int mine = i / top;
             int place = i % top;
             const uint64_t entry = some[mine][place];
@@ -350,7 +471,7 @@ __global__ void __launch_bounds__(kThreads) log_probs_join_kernel(LogProbsArgs a
         }
     }
     __syncthreads();
-    if (threadIdx.x < top) write_entry(a, row, threadIdx.x, best[threadIdx.x], p, log2_S);
+    for (int i = threadIdx.x; i < top; i += THREADS) write_entry(a, row, i, best[i], p, log2_S);
 }
 
 // dx_j = a ([j = t] - p_j) - b p_j (l_j + entropy); a thread has K chunks of a row, and an element of those behind the whole chunks.
@@ -418,8 +539,9 @@ LogProbsPlan plan_log_probs(int64_t rows, int64_t classes, bool bf16, int top)
 
 template <bool BF16, int VEC, int K, bool WAVE> void launch_slices(const LogProbsArgs &a, const LogProbsPlan &p, Part *parts, uint64_t *lists, hipStream_t stream)
 {
-    const int64_t groups = WAVE ? (a.rows + 3) / 4 : a.rows * p.slices;
-    log_probs_slices_kernel<BF16, VEC, K, WAVE><<<static_cast<unsigned>(groups), kThreads, 0, stream>>>(a, p.slice, p.slices, parts, lists);
+    const unsigned groups = static_cast<unsigned>(WAVE ? (a.rows + 3) / 4 : a.rows * p.slices);
+    (a.top ? log_probs_slices_kernel<BF16, VEC, K, WAVE, true> : log_probs_slices_kernel<BF16, VEC, K, WAVE, false>)<<<groups, kThreads, 0, stream>>>(a, p.slice, p.slices, parts,
+                                                                                                                                                   lists);
 }
 
 template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan &p, void *workspace, hipStream_t stream)
@@ -444,7 +566,11 @@ template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan
         else if (p.k == 2) launch_slices<BF16, VEC, 2, true>(b, p, parts, lists, stream);
         else if (p.k == 4) launch_slices<BF16, VEC, 4, true>(b, p, parts, lists, stream);
         else launch_slices<BF16, VEC, 8, true>(b, p, parts, lists, stream);
-        if (p.slices > 1) log_probs_join_kernel<<<static_cast<unsigned>(b.rows), kThreads, 0, stream>>>(b, p.slices, parts, lists);
+        if (p.slices > 1) {
+            const unsigned groups = static_cast<unsigned>(b.rows);
+            if (int64_t(p.slices) * std::max(a.top, 8) <= 512) log_probs_join_kernel<64><<<groups, 64, 0, stream>>>(b, p.slices, parts, lists);
+            else log_probs_join_kernel<256><<<groups, 256, 0, stream>>>(b, p.slices, parts, lists);
+        }
     }
     return hipGetLastError();
 }

@@ -57,21 +57,20 @@ __device__ __forceinline__ uint64_t entry_of(float x, int index) { return uint64
 
 // log S comes as log2 S, and every use of it is one multiply-add, spelled out: the same bits wherever it is.
 __device__ __forceinline__ float log_prob(float x, const Part &p, float log2_S) { return fmaf(-kLn2, log2_S, x - p.c); }
-// what is written of a row
-__device__ __forceinline__ void write_row(const LogProbsArgs &a, int64_t row, const Part &p, float log2_S)
+struct Token {
+    int64_t t;
+    float x;
+};
+__device__ __forceinline__ Token read_token(const LogProbsArgs &a, int64_t row)
 {
-    if (a.logp) {
-        const int64_t t = a.tokens[row];
-        float logp = 0.f;
-        if (t >= a.classes) {
-            logp = __builtin_nanf("");
-        } else if (t >= 0) {
-            const float x = a.bf16 ? Element<true>::get(static_cast<const uint16_t *>(a.logits) + row * a.row_stride + t)
-                                   : static_cast<const float *>(a.logits)[row * a.row_stride + t];
-            logp = p.S == 0.f ? -infinity() : log_prob(x, p, log2_S);
-        }
-        a.logp[row] = logp;
-    }
+    if (!a.logp) return {-1, 0.f};
+    const int64_t t = a.tokens[row], at = row * a.row_stride + (t >= 0 && t < a.classes ? t : 0);
+    return {t, a.bf16 ? Element<true>::get(static_cast<const uint16_t *>(a.logits) + at) : static_cast<const float *>(a.logits)[at]};
+}
+// what is written of a row
+__device__ __forceinline__ void write_row(const LogProbsArgs &a, int64_t row, const Token &token, const Part &p, float log2_S)
+{
+    if (a.logp) a.logp[row] = token.t < 0 ? 0.f : token.t >= a.classes ? __builtin_nanf("") : p.S == 0.f ? -infinity() : log_prob(token.x, p, log2_S);
     if (a.entropy) a.entropy[row] = p.S == 0.f ? 0.f : fmaf(kLn2, log2_S, -(p.E / p.S));
     if (a.largest) {
         // a NaN that the largest value does not show is in the sum
@@ -259,6 +258,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
     __shared__ float meet[3][4];
     __shared__ uint32_t maxima[WAVE || !TOP ? 1 : kThreads];
     __shared__ float bound;
+    __shared__ int ranks[WAVE || !TOP ? 1 : 128];
     const int wave = threadIdx.x / 64, team = WAVE ? wave : 0, lane = threadIdx.x % Group::kSize;
     const int unit = WAVE ? blockIdx.x * kTeams + team : blockIdx.x;               // fewer than 2^22 in a batch
     const int row = WAVE || slices == 1 ? unit : unit / slices;
@@ -272,6 +272,9 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
     typename C::raw raw[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) raw[k] = C::load_once(x + place(k));
+    const bool alone = WAVE || slices == 1;
+    Token token = {};
+    if (alone) token = read_token(a, row);
     float v[VEC], most[K], own = -infinity();            // own: the largest of this thread
 #pragma unroll
     for (int k = 0; k < K; ++k) {
@@ -332,9 +335,8 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
         join_lanes<4>(p);
     }
     const float log2_S = __builtin_amdgcn_logf(p.S);     // the hardware's logarithm is that to base 2
-    const bool alone = WAVE || slices == 1;
     if (lane == 0) {
-        if (alone) write_row(a, row, p, log2_S);
+        if (alone) write_row(a, row, token, p, log2_S);
         else parts[unit] = p;
     }
     if constexpr (TOP) {
@@ -406,12 +408,29 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
             if (alone) write_entry(a, row, rank, entry, p, log2_S);
             else lists[int64_t(unit) * a.top + rank] = entry;
         };
-        for (int i = lane; i < n; i += Group::kSize) {
-            const uint64_t entry = list[i];
-            int rank = 0;
+        if (!WAVE && n <= 128) {
+            // several threads an entry, each against a part of the others
+            const int across = n <= 64 ? 64 : 128, each = (n * across + kThreads - 1) / kThreads, i = threadIdx.x % across, first = threadIdx.x / across * each;
+            if (threadIdx.x < across) ranks[threadIdx.x] = 0;
+            __syncthreads();
+            uint64_t entry = 0;
+            if (i < n) {
+                entry = list[i];
+                int rank = 0;
 #pragma unroll 8
-            for (int j = 0; j < n; ++j) rank += list[j] > entry;
-            if (rank < a.top) leave(rank, entry);
+                for (int j = first; j < min(first + each, n); ++j) rank += list[j] > entry;
+                atomicAdd(&ranks[i], rank);
+            }
+            __syncthreads();
+            if (threadIdx.x < n && ranks[i] < a.top) leave(ranks[i], entry);
+        } else {
+            for (int i = lane; i < n; i += Group::kSize) {
+                const uint64_t entry = list[i];
+                int rank = 0;
+#pragma unroll 8
+                for (int j = 0; j < n; ++j) rank += list[j] > entry;
+                if (rank < a.top) leave(rank, entry);
+            }
         }
         for (int rank = n + lane; rank < a.top; rank += Group::kSize) leave(rank, 0);
     }
@@ -422,11 +441,48 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
 constexpr int kListsAtOnce = 8;
 template <int THREADS> __global__ void __launch_bounds__(THREADS) log_probs_join_kernel(LogProbsArgs a, int slices, const Part *parts, const uint64_t *lists)
 {
-    __shared__ uint64_t some[kListsAtOnce + 1][kMostTop], best[kMostTop];
+    extern __shared__ uint64_t some[];                   // [list][place], the ones found so far first; behind them those that are found
     __shared__ float meet[3][4];
     const int64_t row = blockIdx.x;
+    const int top = a.top;
+    const Token token = read_token(a, row);
     Part p = {-infinity(), 0.f, 0.f, 0.f};
     for (int i = threadIdx.x; i < slices; i += THREADS) p = joined(p, parts[row * slices + i]);
+    uint64_t *best = some + (kListsAtOnce + 1) * top;
+    for (int i = threadIdx.x; i < top; i += THREADS) best[i] = 0;
+    for (int first = 0; first < slices && top > 0; first += kListsAtOnce) {
+        const int now = min(kListsAtOnce, slices - first);
+        __syncthreads();
+        for (int i = threadIdx.x; i < now * top; i += THREADS) some[top + i] = lists[(row * slices + first) * top + i];
+        for (int i = threadIdx.x; i < top; i += THREADS) {
+            some[i] = best[i];
+            best[i] = 0;
+        }
+        __syncthreads();
+        // of `count` lists the first ones of each, `top` or more together, are no smaller than the smallest of the last of these
+        const int empty = first == 0 ? 1 : 0, count = now + 1 - empty, share = (top + count - 1) / count;
+        uint64_t bound = ~uint64_t(0);
+        for (int list = empty; list <= now; ++list) bound = min(bound, some[list * top + share - 1]);
+        for (int i = threadIdx.x; i < count * top; i += THREADS) {
+            const int rank = i / count, mine = empty + i - rank * count;
+            const uint64_t entry = some[mine * top + rank];
+            if (!entry || entry < bound) continue;
+            int before[kListsAtOnce + 1];                // larger ones of each list, all lists a step at a time
+#pragma unroll
+            for (int other = 0; other <= kListsAtOnce; ++other) before[other] = 0;
+            for (int step = 1 << (31 - __builtin_clz(top)); step > 0; step /= 2) {
+#pragma unroll
+                for (int other = 0; other <= kListsAtOnce; ++other) {
+                    const int to = before[other] + step;
+                    if (other >= empty && other <= now && to <= top && some[other * top + to - 1] > entry) before[other] = to;
+                }
+            }
+            int place = rank;
+#pragma unroll
+            for (int other = 0; other <= kListsAtOnce; ++other) place += other == mine ? 0 : before[other];
+            if (place < top) best[place] = entry;
+        }
+    }
     join_lanes<64>(p);
     if constexpr (THREADS > 64) {
         if (threadIdx.x % 64 == 0) {
@@ -438,38 +494,8 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) log_probs_join
         p = {meet[0][threadIdx.x % 4], meet[1][threadIdx.x % 4], meet[2][threadIdx.x % 4], 0.f};
         join_lanes<4>(p);
     }
-    const float log2_S = __builtin_amdgcn_logf(p.S);                 // the hardware's logarithm is that to base 2
-    if (threadIdx.x == 0) write_row(a, row, p, log2_S);
-    const int top = a.top;
-    if (top == 0) return;
-    for (int i = threadIdx.x; i < top; i += THREADS) best[i] = 0;
-    for (int first = 0; first < slices; first += kListsAtOnce) {
-        const int now = min(kListsAtOnce, slices - first);
-        __syncthreads();
-        for (int i = threadIdx.x; i < now * top; i += THREADS) some[1 + i / top][i % top] = lists[(row * slices + first) * top + i];
-        for (int i = threadIdx.x; i < top; i += THREADS) {
-            some[0][i] = best[i];
-            best[i] = 0;
-        }
-        __syncthreads();
-        for (int i = threadIdx.x; i < (now + 1) * top; i += THREADS) {
-            const int mine = i / top;
-            int place = i % top;
-            const uint64_t entry = some[mine][place];
-            if (!entry) continue;
-            for (int other = 0; other <= now; ++other) {
-                if (other == mine) continue;
-                int lo = 0, hi = top;                    // entries before lo are larger, from hi on they are not
-                while (lo < hi) {
-                    const int mid = (lo + hi) / 2;
-                    if (some[other][mid] > entry) lo = mid + 1;
-                    else hi = mid;
-                }
-                place += lo;
-            }
-            if (place < top) best[place] = entry;
-        }
-    }
+    const float log2_S = __builtin_amdgcn_logf(p.S);
+    if (threadIdx.x == 0) write_row(a, row, token, p, log2_S);
     __syncthreads();
     for (int i = threadIdx.x; i < top; i += THREADS) write_entry(a, row, i, best[i], p, log2_S);
 }
@@ -568,8 +594,10 @@ template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan
         else launch_slices<BF16, VEC, 8, true>(b, p, parts, lists, stream);
         if (p.slices > 1) {
             const unsigned groups = static_cast<unsigned>(b.rows);
-            if (int64_t(p.slices) * std::max(a.top, 8) <= 512) log_probs_join_kernel<64><<<groups, 64, 0, stream>>>(b, p.slices, parts, lists);
-            else log_probs_join_kernel<256><<<groups, 256, 0, stream>>>(b, p.slices, parts, lists);
+            const size_t lds = (kListsAtOnce + 2) * size_t(a.top) * 8;
+            // a wavefront where there is little to do: as many rows at once as there are wavefronts
+            if (int64_t(std::min(p.slices, kListsAtOnce) + 1) * a.top <= 128 && p.slices <= 64) log_probs_join_kernel<64><<<groups, 64, lds, stream>>>(b, p.slices, parts, lists);
+            else log_probs_join_kernel<256><<<groups, 256, lds, stream>>>(b, p.slices, parts, lists);
         }
     }
     return hipGetLastError();

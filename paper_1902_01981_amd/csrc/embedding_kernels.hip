@@ -4,10 +4,11 @@
 // positions, and with them the runs, ascend within its stretch.
 //
 //   embedding_forward_kernel   chunks of 16 bytes of the rows of y, side by side
-//   sort_count_kernel, sort_place_kernel   a stable sort by eight bits of the tokens, in as many passes as the vocabulary has bytes
-//   embedding_sums_kernel      pieces of the sorted positions: sums of a cell (a run's token) that lies in a piece go to the gradient, others to the workspace
-//   embedding_join_kernel      cells of several pieces
-//   embedding_zeros_kernel     the rows of the gradient that no position has
+//   sort_few_kernel            a stable sort of the positions by token, nine bits of it or fewer a pass, by one workgroup;
+//   sort_count_kernel, sort_place_kernel   by many, a pair of launches a pass
+//   embedding_sums_kernel, embedding_wide_sums_kernel   pieces of the sorted positions: sums of a cell (a run's token) that lies in a piece go to the
+//                              gradient, others to the workspace
+//   embedding_rest_kernel      cells of several pieces, and the rows of the gradient that no position has
 #include "layers_device.h"
 
 #include <algorithm>
@@ -16,7 +17,7 @@ namespace cr {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 
 // n / d for n < 2^31, by a product
 struct Divisor {
@@ -125,10 +126,10 @@ template <bool BF16, bool TABLE_BF16> void launch_forward(const EmbeddingArgs &a
 }
 
 // ---- the sort --------------------------------------------------------------------------------------------------------------------
-constexpr int kDigits = 256;                             // of a pass
-constexpr int kWaves = kThreads / 64, kKeysOfLane = 16;
-constexpr int kTile = kThreads * kKeysOfLane;            // positions that a workgroup sorts at once: a stretch of 1 024 per wavefront
-constexpr int kMostBlocks = 512;                         // of a pass, each with as many tiles as it takes
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kKeysOfLane = 8;
+constexpr int kTile = kSortThreads * kKeysOfLane;        // positions that a workgroup sorts at once: a stretch of 512 per wavefront
+constexpr int kDigits = 512;                             // of a pass, at most
+constexpr int kMostBlocks = 256;                         // of a pass, each with as many tiles as it takes
 
 // Runs of a batch, by the first of their points in it.
 struct BatchRuns {
@@ -156,95 +157,175 @@ struct SortPass {
     uint8_t *run_out;                                    // of the last pass, if there are several runs
     uint32_t *counts;                                    // [workgroup][digit]
     uint32_t n;                                          // positions
-    int tiles, shift;                                    // tiles of a workgroup
+    int tiles, bits, shift;                              // tiles of a workgroup; bits of a digit
     __device__ __forceinline__ uint32_t key(uint32_t i) const
     {
         if (!tokens) return keys[i];
         const int64_t t = tokens[walk.at(i)];
         return t >= 0 && t < vocabulary ? static_cast<uint32_t>(t) : vocabulary;
     }
+    __device__ __forceinline__ void put(const BatchRuns &runs, uint32_t to, uint32_t k, uint32_t i) const
+    {
+        keys_out[to] = k;
+        order_out[to] = i;
+        if (run_out) run_out[to] = static_cast<uint8_t>(runs.of(static_cast<int>(walk.positions.of(i))));
+    }
 };
 
-__global__ void __launch_bounds__(kThreads) sort_count_kernel(SortPass s, uint64_t *bits, int64_t words)
+// A key's rank among the keys of its wavefront with its digit: those of earlier steps, and of lower lanes.  count[digit]: such keys so far.
+__device__ __forceinline__ uint32_t rank_of(uint32_t digit, int bits, bool is, uint32_t *count)
 {
-    __shared__ uint32_t count[kDigits];
-    for (int64_t w = int64_t(blockIdx.x) * kThreads + threadIdx.x; w < words; w += int64_t(gridDim.x) * kThreads) bits[w] = 0;
-    count[threadIdx.x] = 0;
-    __syncthreads();
-    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * kTile, end = std::min<uint64_t>(begin + uint64_t(s.tiles) * kTile, s.n);
-    for (uint64_t i = begin + threadIdx.x; i < end; i += kThreads) atomicAdd(&count[s.key(static_cast<uint32_t>(i)) >> s.shift & (kDigits - 1)], 1u);
-    __syncthreads();
-    s.counts[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
-}
-
-// A key's place: keys with smaller digits, keys with its digit in earlier workgroups, in earlier tiles, wavefronts, and steps of its wavefront, and in
-// lower lanes.
-__global__ void __launch_bounds__(kThreads) sort_place_kernel(SortPass s, BatchRuns runs)
-{
-    __shared__ uint32_t place[kWaves][kDigits], totals[kWaves];
-    const int digit = threadIdx.x, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    uint32_t total = 0, before = 0;
-    for (unsigned b = 0; b < gridDim.x; ++b) {
-        const uint32_t c = s.counts[b * kDigits + digit];
-        if (b < blockIdx.x) before += c;
-        total += c;
+    const int lane = threadIdx.x % 64;
+    uint64_t same = __ballot(is);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t set = __ballot(digit >> b & 1);
+        same &= digit >> b & 1 ? set : ~set;
     }
-    uint32_t sum = total;                                // inclusive over the digits
+    const int leader = is ? __ffsll(static_cast<long long>(same)) - 1 : lane;
+    uint32_t old = 0;
+    if (is && lane == leader) old = atomicAdd(&count[digit], static_cast<uint32_t>(__popcll(same)));
+    return __shfl(old, leader) + __popcll(same & ((uint64_t(1) << lane) - 1));
+}
+// The sum of `mine` over the digits before this thread's, a digit each of the first kDigits threads; sums: a place for each of their wavefronts.
+__device__ __forceinline__ uint32_t digits_before(uint32_t mine, uint32_t *sums)
+{
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    uint32_t sum = mine;                                 // up to and with this digit
     for (int d = 1; d < 64; d *= 2) {
         const uint32_t other = __shfl_up(sum, d);
         if (lane >= d) sum += other;
     }
-    if (lane == 63) totals[wave] = sum;
+    if (lane == 63 && wave < kDigits / 64) sums[wave] = sum;
     __syncthreads();
-    uint32_t next = before + sum - total;                // the place of the next key with this thread's digit
-    for (int w = 0; w < wave; ++w) next += totals[w];
+    uint32_t before = sum - mine;
+    for (int w = 0; w < std::min(wave, kDigits / 64); ++w) before += sums[w];
+    return before;
+}
+
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortPass s, uint64_t *bits, int64_t words)
+{
+    __shared__ uint32_t count[kDigits];
+    for (int64_t w = int64_t(blockIdx.x) * kSortThreads + threadIdx.x; w < words; w += int64_t(gridDim.x) * kSortThreads) bits[w] = 0;
+    if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
+    __syncthreads();
+    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * kTile, end = std::min<uint64_t>(begin + uint64_t(s.tiles) * kTile, s.n);
+    for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&count[s.key(static_cast<uint32_t>(i)) >> s.shift & ((1u << s.bits) - 1)], 1u);
+    __syncthreads();
+    if (threadIdx.x < kDigits) s.counts[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
+}
+
+// A key's place: keys with smaller digits, keys with its digit in earlier workgroups, in earlier tiles and wavefronts, and its rank in its own.
+__global__ void __launch_bounds__(kSortThreads) sort_place_kernel(SortPass s, BatchRuns runs)
+{
+    __shared__ uint32_t place[kSortWaves][kDigits], sums[kDigits / 64], halves[2][kDigits];
+    const int digit = threadIdx.x % kDigits, half = threadIdx.x / kDigits, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const uint32_t mask = (1u << s.bits) - 1;
+    static_assert(kSortThreads == 2 * kDigits);
+    uint32_t total = 0, before = 0;
+    constexpr int U = 8;
+    for (unsigned b = half; b < gridDim.x; b += 2 * U) {
+        uint32_t c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) c[u] = s.counts[std::min(b + 2 * u, gridDim.x - 1) * kDigits + digit];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            total += b + 2 * u < gridDim.x ? c[u] : 0;
+            before += b + 2 * u < blockIdx.x ? c[u] : 0;
+        }
+    }
+    if (half) {
+        halves[0][digit] = total;
+        halves[1][digit] = before;
+    }
+    __syncthreads();
+    if (!half) {
+        total += halves[0][digit];
+        before += halves[1][digit];
+    }
+    uint32_t next = before + digits_before(total, sums); // the place of the next key with this thread's digit, in the first kDigits threads
 
     const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * kTile;
     for (int tile = 0; tile < s.tiles; ++tile) {
         const uint64_t first = begin + uint64_t(tile) * kTile;
         if (first >= s.n) break;
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) place[w][digit] = 0;
+        for (int w = half; w < kSortWaves; w += 2) place[w][digit] = 0;
         __syncthreads();
         uint32_t key[kKeysOfLane], order[kKeysOfLane], rank[kKeysOfLane];
+        const uint64_t own = first + wave * (kTile / kSortWaves) + lane;
 #pragma unroll
         for (int u = 0; u < kKeysOfLane; ++u) {
-            const uint64_t i = first + wave * (kTile / kWaves) + u * 64 + lane;
-            const uint32_t j = static_cast<uint32_t>(std::min<uint64_t>(i, s.n - 1));
+            const uint32_t j = static_cast<uint32_t>(std::min<uint64_t>(own + u * 64, s.n - 1));
             key[u] = s.key(j);
             order[u] = s.tokens ? j : s.order[j];
         }
 #pragma unroll
-        for (int u = 0; u < kKeysOfLane; ++u) {
-            const bool is = first + wave * (kTile / kWaves) + u * 64 + lane < s.n;
-            const uint32_t d = key[u] >> s.shift & (kDigits - 1);
-            uint64_t same = __ballot(is);
-#pragma unroll
-            for (int b = 0; b < 8; ++b) {
-                const uint64_t set = __ballot(d >> b & 1);
-                same &= d >> b & 1 ? set : ~set;
+        for (int u = 0; u < kKeysOfLane; ++u) rank[u] = rank_of(key[u] >> s.shift & mask, s.bits, own + u * 64 < s.n, place[wave]);
+        __syncthreads();
+        if (!half)
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = place[w][digit];
+                place[w][digit] = next;
+                next += c;
             }
-            const int leader = is ? __ffsll(static_cast<long long>(same)) - 1 : lane;
-            uint32_t old = 0;
-            if (is && lane == leader) old = atomicAdd(&place[wave][d], static_cast<uint32_t>(__popcll(same)));
-            rank[u] = __shfl(old, leader) + __popcll(same & ((uint64_t(1) << lane) - 1));
-        }
         __syncthreads();
-        for (int w = 0; w < kWaves; ++w) {
-            const uint32_t c = place[w][digit];
-            place[w][digit] = next;
-            next += c;
-        }
+#pragma unroll
+        for (int u = 0; u < kKeysOfLane; ++u)
+            if (own + u * 64 < s.n) s.put(runs, place[wave][key[u] >> s.shift & mask] + rank[u], key[u], order[u]);
+    }
+}
+
+// Positions that one workgroup holds: all passes in one launch.
+__global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortPass s, BatchRuns runs, int passes, uint64_t *bits, int64_t words)
+{
+    __shared__ uint32_t place[kSortWaves][kDigits], sums[kDigits / 64], keys[kTile];
+    __shared__ uint16_t orders[kTile];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, own = wave * (kTile / kSortWaves) + lane, n = static_cast<int>(s.n);
+    const uint32_t mask = (1u << s.bits) - 1;
+    for (int64_t w = threadIdx.x; w < words; w += kSortThreads) bits[w] = 0;
+    uint32_t key[kKeysOfLane], rank[kKeysOfLane];
+    int order[kKeysOfLane];
+#pragma unroll
+    for (int u = 0; u < kKeysOfLane; ++u) {
+        order[u] = own + u * 64;
+        key[u] = s.key(std::min(own + u * 64, n - 1));
+    }
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * s.bits;
+        for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) place[i / kDigits][i % kDigits] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kKeysOfLane; ++u) rank[u] = rank_of(key[u] >> shift & mask, s.bits, own + u * 64 < n, place[wave]);
+        __syncthreads();
+        uint32_t total = 0;
+        if (threadIdx.x < kDigits)
+            for (int w = 0; w < kSortWaves; ++w) total += place[w][threadIdx.x];
+        uint32_t next = digits_before(total, sums);
+        if (threadIdx.x < kDigits)
+            for (int w = 0; w < kSortWaves; ++w) {
+                const uint32_t c = place[w][threadIdx.x];
+                place[w][threadIdx.x] = next;
+                next += c;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < kKeysOfLane; ++u)
+            if (own + u * 64 < n) {
+                const uint32_t to = place[wave][key[u] >> shift & mask] + rank[u];
+                keys[to] = key[u];
+                orders[to] = static_cast<uint16_t>(order[u]);
+            }
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kKeysOfLane; ++u) {
-            if (first + wave * (kTile / kWaves) + u * 64 + lane >= s.n) continue;
-            const uint32_t to = place[wave][key[u] >> s.shift & (kDigits - 1)] + rank[u];
-            s.keys_out[to] = key[u];
-            s.order_out[to] = order[u];
-            if (s.run_out) s.run_out[to] = static_cast<uint8_t>(runs.of(static_cast<int>(s.walk.positions.of(order[u]))));
+            key[u] = keys[std::min(own + u * 64, n - 1)];
+            order[u] = orders[std::min(own + u * 64, n - 1)];
         }
+        __syncthreads();
     }
+#pragma unroll
+    for (int u = 0; u < kKeysOfLane; ++u)
+        if (own + u * 64 < n) s.put(runs, own + u * 64, key[u], order[u]);
 }
 
 // ---- the sums --------------------------------------------------------------------------------------------------------------------
@@ -273,8 +354,9 @@ struct Gradient {
 };
 
 constexpr int kRowsAtOnce = 8;
+template <int VEC> __device__ __forceinline__ int chunk_of(int q, int nq, int channels) { return q < nq - 1 ? q * VEC : channels - VEC; }
 
-// TS lanes per piece, each with a chunk of the channels; a wavefront per piece and 64 chunks where there are more.
+// TS lanes per piece, each with a chunk of the channels, for rows of up to 32 chunks.
 template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads) embedding_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs)
 {
     using C = Chunk<BF16, VEC>;
@@ -339,12 +421,95 @@ template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads
     }
 }
 
+// Wider rows: a wavefront per piece and 64 chunks.  Its lanes look up 64 positions at once, what is at them is a scalar then; a row's place in the registers
+// takes the row eight further on as soon as it is added.
+template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedding_wide_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    const int lane = threadIdx.x % 64;
+    const uint64_t teams = uint64_t(s.pieces) * slabs;
+    for (uint64_t team = uint64_t(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); team < teams; team += uint64_t(gridDim.x) * (kThreads / 64)) {
+        const unsigned piece = static_cast<unsigned>(team / slabs);
+        const int q = static_cast<int>(team % slabs) * 64 + lane;
+        const uint32_t begin = piece * s.length, end = min(begin + s.length, s.n);
+        const int at = chunk_of<VEC>(min(q, nq - 1), nq, g.channels);
+        const unsigned lane_byte = at * sizeof(T);       // channels of 2^24 at most
+        // 64 positions: a lane's own, and before which of them another cell begins
+        struct Look {
+            uint32_t key, run;
+            int64_t offset;
+            uint64_t border;
+        };
+        auto look = [&](uint32_t first) {
+            const uint32_t i = min(first + lane, end - 1);
+            Look l;
+            const Cell own = cell_at(s, i), before = cell_at(s, max(i, 1u) - 1);
+            l.key = own.key;
+            l.run = own.run;
+            l.offset = g.walk.at(s.order[i]);
+            l.border = __ballot(first + lane < end && i > begin && !(own == before));
+            return l;
+        };
+        Look ahead = look(begin), here = ahead;
+        Cell now = {static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(ahead.key)), static_cast<uint32_t>(__builtin_amdgcn_readfirstlane(ahead.run))};
+        if (now.key >= s.vocabulary) continue;           // nothing but positions without a row from here on
+        bool begun = begin == 0 || !(cell_at(s, begin - 1) == now);
+        float acc[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+        auto leave = [&](bool ends) {
+            if (now.key >= s.vocabulary) return;
+            if (begun && q == 0) atomicOr(reinterpret_cast<unsigned long long *>(g.bits + now.run * g.words + now.key / 64), 1ull << now.key % 64);
+            const bool whole = begun && ends;
+            float *to = whole ? g.dtable + (int64_t(now.run) * s.vocabulary + now.key) * g.channels : g.parts + (2 * int64_t(piece) + begun) * g.channels;
+            const float by = whole ? g.scale : 1.f;
+            float v[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = acc[i] * by;
+            if (q < nq) store_row<false, VEC>(to, at, v);
+        };
+        typename C::raw raw[kRowsAtOnce];
+        auto fetch = [&](int u, int of) {                // the row of position `of` of the 64 ahead
+            const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(ahead.offset), of), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(ahead.offset >> 32), of);
+            const char *row = static_cast<const char *>(g.dy) + static_cast<int64_t>(uint64_t(hi) << 32 | lo) * static_cast<int64_t>(sizeof(T));
+            raw[u] = C::load(reinterpret_cast<const T *>(scalar(row) + lane_byte));
+        };
+#pragma unroll
+        for (int u = 0; u < kRowsAtOnce; ++u) fetch(u, u);
+        const int steps = (end - begin + kRowsAtOnce - 1) / kRowsAtOnce;
+        for (int step = 0; step < steps; ++step) {
+            const int first = step * kRowsAtOnce % 64;   // of the 64 here
+            if (first == 0) here = ahead;
+            if (first == 64 - kRowsAtOnce && step + 1 < steps) ahead = look(begin + (step + 1) * kRowsAtOnce);
+#pragma unroll
+            for (int u = 0; u < kRowsAtOnce; ++u) {
+                const int e = first + u;
+                if (begin + step * kRowsAtOnce + u < end) {
+                    if (here.border >> e & 1) {
+                        leave(true);
+                        now = {static_cast<uint32_t>(__builtin_amdgcn_readlane(here.key, e)), static_cast<uint32_t>(__builtin_amdgcn_readlane(here.run, e))};
+                        begun = true;
+#pragma unroll
+                        for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+                    }
+                    float v[VEC];
+                    C::widen(raw[u], v);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[i] += v[i];
+                }
+                if (step + 1 < steps) fetch(u, (e + kRowsAtOnce) % 64);
+            }
+        }
+        leave(end == s.n || !(cell_at(s, end) == now));
+    }
+}
+
 // The cell that begins in a piece and goes on behind it: its parts, added up in 64 bits.
-__global__ void __launch_bounds__(kThreads) embedding_join_kernel(Gradient g, Sorted s)
+__device__ __forceinline__ void join_cell(const Gradient &g, const Sorted &s, unsigned piece, int part, int parts)
 {
     __shared__ double meet[kWaves][64 * 4];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const unsigned piece = blockIdx.x;
     const uint32_t begin = piece * s.length, end = min(begin + s.length, s.n);
     if (end == s.n) return;
     const Cell now = cell_at(s, end - 1);
@@ -357,7 +522,7 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(Gradient g, So
         more += count;
         if (count < kThreads) break;
     }
-    for (int64_t c0 = int64_t(blockIdx.y) * 256; c0 < g.channels; c0 += int64_t(gridDim.y) * 256) {
+    for (int64_t c0 = int64_t(part) * 256; c0 < g.channels; c0 += int64_t(parts) * 256) {
         double sum[4] = {};
         constexpr int U = 4;
         for (unsigned p = wave; p <= more; p += U * kWaves) {
@@ -386,35 +551,52 @@ __global__ void __launch_bounds__(kThreads) embedding_join_kernel(Gradient g, So
     }
 }
 
-// Rows without positions, a few neighbours at a time; bits null: all rows.
-__global__ void __launch_bounds__(kThreads) embedding_zeros_kernel(float *dtable, int channels, int vocabulary, int runs, const uint64_t *bits, int64_t words, int neighbours)
+// Rows without positions, `neighbours` at a time; bits null: all rows.
+struct Zeros {
+    float *dtable;
+    int channels, vocabulary, runs, neighbours, parts;   // parts: workgroups that share such rows
+    const uint64_t *bits;
+    int64_t words, workgroups;
+};
+__device__ __forceinline__ void clear_rows(const Zeros &z, int64_t workgroup)
 {
     const f4 none = {0.f, 0.f, 0.f, 0.f};
-    const int64_t groups = (vocabulary + neighbours - 1) / neighbours, all = groups * runs;
-    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    const int part = static_cast<int>(workgroup % z.parts);
+    const int64_t groups = (z.vocabulary + z.neighbours - 1) / z.neighbours, all = groups * z.runs, others = z.workgroups / z.parts;
+    for (int64_t i = workgroup / z.parts; i < all; i += others) {
         const int64_t run = i / groups;
-        const int first = static_cast<int>(i - run * groups) * neighbours, count = min(neighbours, vocabulary - first);
-        float *rows = dtable + (run * vocabulary + first) * channels;
-        uint64_t have = bits ? bits[run * words + first / 64] >> first % 64 : 0;
+        const int first = static_cast<int>(i - run * groups) * z.neighbours, count = min(z.neighbours, z.vocabulary - first);
+        float *rows = z.dtable + (run * z.vocabulary + first) * z.channels;
+        uint64_t have = z.bits ? z.bits[run * z.words + first / 64] >> first % 64 : 0;
         if (count < 64) have &= (uint64_t(1) << count) - 1;
         auto clear = [&](float *from, int64_t floats) {
             const int64_t whole = floats / 4;
-            for (int64_t c = int64_t(blockIdx.y) * kThreads + threadIdx.x; c < whole; c += int64_t(gridDim.y) * kThreads) Chunk<false, 4>::store(from + 4 * c, none);
-            if (blockIdx.y == 0 && threadIdx.x < floats - 4 * whole) from[4 * whole + threadIdx.x] = 0.f;
+            for (int64_t c = int64_t(part) * kThreads + threadIdx.x; c < whole; c += int64_t(z.parts) * kThreads) Chunk<false, 4>::store(from + 4 * c, none);
+            if (part == 0 && threadIdx.x < floats - 4 * whole) from[4 * whole + threadIdx.x] = 0.f;
         };
         if (have == 0) {
-            clear(rows, int64_t(count) * channels);
+            clear(rows, int64_t(count) * z.channels);
         } else {
             for (int r = 0; r < count; ++r)
-                if (!(have >> r & 1)) clear(rows + int64_t(r) * channels, channels);
+                if (!(have >> r & 1)) clear(rows + int64_t(r) * z.channels, z.channels);
         }
     }
+}
+// What is left once the sums are there: cells of several pieces, and rows of none.  The two share no row.
+__global__ void __launch_bounds__(kThreads) embedding_rest_kernel(Gradient g, Sorted s, Zeros z, unsigned joins, int parts)
+{
+    if (blockIdx.x >= joins) {
+        clear_rows(z, blockIdx.x - joins);
+        return;
+    }
+    const int64_t all = int64_t(s.pieces) * parts;
+    for (int64_t i = blockIdx.x; i < all; i += joins) join_cell(g, s, static_cast<unsigned>(i / parts), static_cast<int>(i % parts), parts);
 }
 
 // ---- what a gradient needs -------------------------------------------------------------------------------------------------------
 struct GradPlan {
     uint32_t n;                  // positions of the largest batch of runs
-    int passes;
+    int passes, digit_bits;      // of the sort; of a digit of it
     int vec, nq, team;           // channels of a chunk, chunks of a row, lanes of a piece
     unsigned slabs;
     int64_t words;               // of bits, per run
@@ -433,7 +615,10 @@ GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *b
 {
     GradPlan p = {};
     p.n = n;
-    for (p.passes = 1; p.passes < 4 && (uint64_t(vocabulary) >> (8 * p.passes)) != 0; ++p.passes) {}
+    int bits = 1;                                        // that the numbers 0 to `vocabulary` take
+    while (uint64_t(vocabulary) >> bits) ++bits;
+    p.passes = (bits + 8) / 9;
+    p.digit_bits = (bits + p.passes - 1) / p.passes;
     p.vec = shape.bf16 ? 8 : 4;
     if (shape.channels < p.vec) p.vec = 1;
     p.nq = (shape.channels + p.vec - 1) / p.vec;
@@ -481,17 +666,21 @@ template <bool BF16, int VEC> void launch_sums(const Gradient &g, const Sorted &
     if constexpr (VEC > 1) {                             // rows of single channels are shorter
         if (p.team == 16) go(embedding_sums_kernel<BF16, VEC, 16>, 16);
         else if (p.team == 32) go(embedding_sums_kernel<BF16, VEC, 32>, 32);
-        else go(embedding_sums_kernel<BF16, VEC, 64>, 64);
+        else go(embedding_wide_sums_kernel<BF16, VEC>, 64);
     }
 }
 
-void launch_zeros(const EmbeddingGradArgs &a, float *dtable, int runs, const uint64_t *bits, int64_t words, hipStream_t stream)
+// cells: of several pieces may be among the positions
+void launch_rest(const EmbeddingGradArgs &a, const Gradient &g, const Sorted &s, int runs, bool cells, hipStream_t stream)
 {
-    int neighbours = 64;                                 // at most 64 KB of a workgroup
-    while (neighbours > 1 && int64_t(neighbours) * a.shape.channels > 16384) neighbours /= 2;
-    const int64_t groups = (int64_t(a.vocabulary) + neighbours - 1) / neighbours * runs;
-    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(groups, 1 << 20)), std::max(1, std::min(1024, a.shape.channels / 16384)));
-    embedding_zeros_kernel<<<grid, kThreads, 0, stream>>>(dtable, a.shape.channels, a.vocabulary, runs, bits, words, neighbours);
+    Zeros z = {g.dtable, a.shape.channels, a.vocabulary, runs, 64, 1, g.bits, g.words, 0};
+    while (z.neighbours > 1 && int64_t(z.neighbours) * z.channels > 16384) z.neighbours /= 2;          // at most 64 KB of a workgroup
+    z.parts = std::max(1, std::min(1024, z.channels / 16384));
+    const int64_t groups = (int64_t(a.vocabulary) + z.neighbours - 1) / z.neighbours * runs;
+    z.workgroups = std::min<int64_t>(groups, (1 << 20) / z.parts) * z.parts;
+    const int parts = std::min((a.shape.channels + 255) / 256, 64);
+    const unsigned joins = cells ? static_cast<unsigned>(std::min<int64_t>(int64_t(s.pieces) * parts, 1 << 22)) : 0;
+    embedding_rest_kernel<<<joins + static_cast<unsigned>(z.workgroups), kThreads, 0, stream>>>(g, s, z, joins, parts);
 }
 
 }  // namespace
@@ -527,7 +716,8 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
         float *dtable = a.dtable + int64_t(r0) * a.vocabulary * shape.channels;
         const uint32_t n = static_cast<uint32_t>((a.bounds[r0 + runs.runs] - first) * shape.positions);
         if (n == 0) {
-            launch_zeros(a, dtable, runs.runs, nullptr, 0, stream);
+            const Gradient none = {nullptr, Walk(a.dy, shape.positions), shape.channels, a.scale, dtable, nullptr, nullptr, 0};
+            launch_rest(a, none, Sorted(), runs.runs, false, stream);
             continue;
         }
         const GradPlan p = plan_gradient(shape, a.vocabulary, a.bounds, a.runs, n);
@@ -536,16 +726,22 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
         uint64_t *bits = reinterpret_cast<uint64_t *>(ws + p.bits);
         const unsigned blocks = blocks_of(n);
         const int tiles = static_cast<int>(((uint64_t(n) + kTile - 1) / kTile + blocks - 1) / blocks);
-        for (int pass = 0; pass < p.passes; ++pass) {
+        int end = 0;                                     // of the two buffers, the one that holds the sorted positions
+        for (int pass = 0; pass < (blocks == 1 ? 1 : p.passes); ++pass) {
             const int to = pass % 2, from = 1 - to;
-            const bool last = pass == p.passes - 1;
+            const bool last = blocks == 1 || pass == p.passes - 1;
             const SortPass s = {pass == 0 ? static_cast<const int64_t *>(a.tokens.p) + first * a.tokens.point_stride : nullptr, Walk(a.tokens, shape.positions),
                                 static_cast<uint32_t>(a.vocabulary), words(p.keys[from]), words(p.order[from]), words(p.keys[to]), words(p.order[to]),
-                                last && a.runs > 1 ? reinterpret_cast<uint8_t *>(ws + p.run) : nullptr, words(p.counts), n, tiles, 8 * pass};
-            sort_count_kernel<<<blocks, kThreads, 0, stream>>>(s, bits, pass == 0 ? p.words * runs.runs : 0);
-            sort_place_kernel<<<blocks, kThreads, 0, stream>>>(s, runs);
+                                last && a.runs > 1 ? reinterpret_cast<uint8_t *>(ws + p.run) : nullptr, words(p.counts), n, tiles, p.digit_bits, p.digit_bits * pass};
+            if (blocks == 1) {
+                sort_few_kernel<<<1, kSortThreads, 0, stream>>>(s, runs, p.passes, bits, p.words * runs.runs);
+            } else {
+                sort_count_kernel<<<blocks, kSortThreads, 0, stream>>>(s, bits, pass == 0 ? p.words * runs.runs : 0);
+                sort_place_kernel<<<blocks, kSortThreads, 0, stream>>>(s, runs);
+            }
+            end = to;
         }
-        const int end = (p.passes - 1) % 2, length = piece_length(n, p.team, p.slabs);
+        const int length = piece_length(n, p.team, p.slabs);
         const Sorted s = {words(p.keys[end]), words(p.order[end]), a.runs > 1 ? reinterpret_cast<const uint8_t *>(ws + p.run) : nullptr, n,
                           static_cast<uint32_t>(a.vocabulary), length, static_cast<unsigned>((uint64_t(n) + length - 1) / length)};
         const size_t e = shape.bf16 ? 2 : 4;
@@ -554,8 +750,7 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
         if (p.vec == 1) shape.bf16 ? launch_sums<true, 1>(g, s, p, stream) : launch_sums<false, 1>(g, s, p, stream);
         else if (shape.bf16) launch_sums<true, 8>(g, s, p, stream);
         else launch_sums<false, 4>(g, s, p, stream);
-        if (s.pieces > 1) embedding_join_kernel<<<dim3(s.pieces, std::min((shape.channels + 255) / 256, 1024)), kThreads, 0, stream>>>(g, s);
-        launch_zeros(a, dtable, runs.runs, bits, p.words, stream);
+        launch_rest(a, g, s, runs.runs, s.pieces > 1, stream);
     }
     return hipGetLastError();
 }

@@ -16,7 +16,7 @@ namespace cr {
 
 namespace {
 
-constexpr int kThreads = 256, kMostTop = 128;
+constexpr int kThreads = 256, kTeam = 256, kMostTop = 128;
 constexpr float kLowest = -3.4028234663852886e38f;
 
 struct Part {
@@ -87,28 +87,35 @@ __device__ __forceinline__ void write_entry(const LogProbsArgs &a, int64_t row, 
 }
 
 // The team that has a row or slice: a wavefront, or a workgroup.
-template <bool WAVE> struct Team {
-    static constexpr int kSize = WAVE ? 64 : kThreads;
+template <int SIZE> struct Team {
+    static constexpr bool kWave = SIZE == 64;
+    static constexpr int kWaves = SIZE / 64;
     static __device__ __forceinline__ void sync()
     {
-        if constexpr (WAVE) {
+        if constexpr (kWave) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
         } else {
             __syncthreads();
         }
     }
+    // f over the team's wavefronts, each of which has a value of its own; meet: a place for each
+    template <typename F> static __device__ __forceinline__ float over_waves(float v, float *meet, F f)
+    {
+        if constexpr (!kWave) {
+            if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = v;
+            __syncthreads();
+            v = meet[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) v = f(v, meet[w]);
+            __syncthreads();
+        }
+        return v;
+    }
     // the sum over the team of small numbers
     static __device__ __forceinline__ int total(int mine, float *meet)
     {
-        float sum = lanes_total<64>(static_cast<float>(mine));
-        if constexpr (!WAVE) {
-            if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = sum;
-            __syncthreads();
-            sum = meet[0] + meet[1] + meet[2] + meet[3];
-            __syncthreads();
-        }
-        return static_cast<int>(sum);
+        return static_cast<int>(over_waves(lanes_total<64>(static_cast<float>(mine)), meet, [](float a, float b) { return a + b; }));
     }
 };
 
@@ -157,12 +164,12 @@ constexpr int kWaveEntries = 512, kBlockEntries = 1024;  // that a team keeps of
 // The `top` largest of chunks [begin, end) of a row, where too many are no smaller than `least`, equal ones mostly: the top-th largest value itself, which is the
 // smallest of them if all the others are too few, and is found bit by bit if not; then as many of its places as are wanted, lowest first.  The chunks are
 // read again each time: 32 KB at most, from the caches.
-template <bool BF16, int VEC, bool WAVE>
+template <bool BF16, int VEC, int TEAM>
 __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::element *x, int begin, int end, int nq, int classes, int top, float least, uint64_t *list, int *count, float *meet)
 {
     using C = Chunk<BF16, VEC>;
-    using Group = Team<WAVE>;
-    const int lane = threadIdx.x % Group::kSize, doubled = nq * VEC - classes;
+    using Group = Team<TEAM>;
+    const int lane = threadIdx.x % TEAM, doubled = nq * VEC - classes;
     // f(number in order, index, value) for the elements of a step that are this thread's; places of a step lie behind those of the one before
     auto of_step = [&](int q0, auto &&f) {
         const int q = q0 + lane;
@@ -176,19 +183,13 @@ __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::elem
     };
     auto number = [&](auto &&counts) {
         int mine = 0;
-        for (int q0 = begin; q0 < end; q0 += Group::kSize) of_step(q0, [&](uint32_t o, int, float) { mine += counts(o); });
+        for (int q0 = begin; q0 < end; q0 += TEAM) of_step(q0, [&](uint32_t o, int, float) { mine += counts(o); });
         return Group::total(mine, meet);
     };
     Group::sync();
     float smallest = infinity();
-    for (int q0 = begin; q0 < end; q0 += Group::kSize) of_step(q0, [&](uint32_t, int, float v) { smallest = v >= least ? fminf(smallest, v) : smallest; });
-    smallest = -lanes_most<64>(-smallest);
-    if constexpr (!WAVE) {
-        if (threadIdx.x % 64 == 0) meet[threadIdx.x / 64] = smallest;
-        __syncthreads();
-        smallest = fminf(fminf(meet[0], meet[1]), fminf(meet[2], meet[3]));
-        __syncthreads();
-    }
+    for (int q0 = begin; q0 < end; q0 += TEAM) of_step(q0, [&](uint32_t, int, float v) { smallest = v >= least ? fminf(smallest, v) : smallest; });
+    smallest = Group::over_waves(-lanes_most<64>(-smallest), meet, [](float a, float b) { return fminf(a, b); });
     uint32_t value = ordered(smallest);
     if (number([&](uint32_t o) { return o > value; }) >= top) {
         value = 0;
@@ -199,7 +200,7 @@ __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::elem
     }
     if (lane == 0) *count = 0;
     Group::sync();
-    for (int q0 = begin; q0 < end; q0 += Group::kSize)
+    for (int q0 = begin; q0 < end; q0 += TEAM)
         of_step(q0, [&](uint32_t o, int index, float v) {
             if (o > value) {
                 const int to = atomicAdd(count, 1);
@@ -208,7 +209,7 @@ __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::elem
         });
     Group::sync();
     int n = min(*count, top);                            // fewer than `top`; places of the value itself fill them up
-    for (int q0 = begin; q0 < end && n < top; q0 += Group::kSize) {
+    for (int q0 = begin; q0 < end && n < top; q0 += TEAM) {
         int mine = 0;
         of_step(q0, [&](uint32_t o, int, float) { mine += o == value; });
         int sum = mine;                                  // up to and with this lane
@@ -217,11 +218,11 @@ __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::elem
             if (static_cast<int>(threadIdx.x % 64) >= d) sum += other;
         }
         int total = __shfl(sum, 63), before = 0;
-        if constexpr (!WAVE) {
+        if constexpr (!Group::kWave) {
             if (threadIdx.x % 64 == 63) meet[threadIdx.x / 64] = static_cast<float>(sum);
             __syncthreads();
             total = 0;
-            for (int w = 0; w < 4; ++w) {
+            for (int w = 0; w < Group::kWaves; ++w) {
                 if (w < static_cast<int>(threadIdx.x / 64)) before += static_cast<int>(meet[w]);
                 total += static_cast<int>(meet[w]);
             }
@@ -245,29 +246,30 @@ __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::elem
 // Arithmetic bounds it as much as reads do (an exponential is four operations), so a sweep over a lane's chunks has no operation too many: the largest first, then
 // the sums, E without a bound on the distances: where a class cannot be it is NaN (0 times infinity), and those lanes add up once more.
 constexpr int kWavesOf[2] = {6, 8};                      // of a SIMD: where a lane has eight chunks, and where it has fewer
-template <bool BF16, int VEC, int K, bool WAVE, bool TOP>
-__global__ void __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kWavesOf[K < 8])))
+template <bool BF16, int VEC, int K, int TEAM, bool TOP>
+__global__ void __launch_bounds__(TEAM == 64 ? kThreads : TEAM) __attribute__((amdgpu_waves_per_eu(kWavesOf[K < 8])))
 log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint64_t *lists)
 {
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
-    using Group = Team<WAVE>;
-    constexpr int kTeams = kThreads / Group::kSize, kEntries = !TOP ? 1 : WAVE ? kWaveEntries : kBlockEntries;
+    using Group = Team<TEAM>;
+    constexpr bool WAVE = Group::kWave;
+    constexpr int kTeams = WAVE ? kThreads / 64 : 1, kEntries = !TOP ? 1 : WAVE ? kWaveEntries : kBlockEntries;
     __shared__ uint64_t entries[kTeams][kEntries];
     __shared__ int counts[kTeams];
-    __shared__ float meet[3][4];
-    __shared__ uint32_t maxima[WAVE || !TOP ? 1 : kThreads];
+    __shared__ float meet[3][Group::kWaves];
+    __shared__ uint32_t maxima[WAVE || !TOP ? 1 : TEAM];
     __shared__ float bound;
     __shared__ int ranks[WAVE || !TOP ? 1 : 128];
-    const int wave = threadIdx.x / 64, team = WAVE ? wave : 0, lane = threadIdx.x % Group::kSize;
+    const int wave = threadIdx.x / 64, team = WAVE ? wave : 0, lane = threadIdx.x % TEAM;
     const int unit = WAVE ? blockIdx.x * kTeams + team : blockIdx.x;               // fewer than 2^22 in a batch
     const int row = WAVE || slices == 1 ? unit : unit / slices;
     if (row >= a.rows) return;                           // whole teams; there is no barrier of the workgroup where a team is a wavefront
     const int nq = (a.classes + VEC - 1) / VEC, begin = WAVE ? 0 : (unit - row * slices) * slice, end = min(begin + slice, nq);
     const int doubled = nq * VEC - a.classes;            // of the last chunk, which is moved back to end with the row
     const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
-    auto place = [&](int k) { return chunk_at<VEC>(min(begin + lane + k * Group::kSize, end - 1), nq, a.classes); };
-    auto has = [&](int k) { return begin + lane + k * Group::kSize < end; };
+    auto place = [&](int k) { return chunk_at<VEC>(min(begin + lane + k * TEAM, end - 1), nq, a.classes); };
+    auto has = [&](int k) { return begin + lane + k * TEAM < end; };
 
     typename C::raw raw[K];
 #pragma unroll
@@ -279,7 +281,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         // what the neighbour has is here a class that cannot be
-        if (begin + lane + k * Group::kSize == nq - 1 && doubled > 0) {
+        if (begin + lane + k * TEAM == nq - 1 && doubled > 0) {
             C::widen(raw[k], v);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) v[i] = i < doubled ? -infinity() : v[i];
@@ -331,8 +333,9 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
         }
         if constexpr (TOP) maxima[threadIdx.x] = short_key(own);
         __syncthreads();
-        p = {meet[0][threadIdx.x % 4], meet[1][threadIdx.x % 4], meet[2][threadIdx.x % 4], 0.f};
-        join_lanes<4>(p);
+        const int w = threadIdx.x % Group::kWaves;
+        p = {meet[0][w], meet[1][w], meet[2][w], 0.f};
+        join_lanes<Group::kWaves>(p);
     }
     const float log2_S = __builtin_amdgcn_logf(p.S);     // the hardware's logarithm is that to base 2
     if (lane == 0) {
@@ -369,9 +372,9 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
             }
             least = key ? unordered(key << 16) : kLowest;
         } else if (wave == 0) {
-            uint32_t keys[4];
+            uint32_t keys[Group::kWaves];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) keys[i] = maxima[threadIdx.x + 64 * i];
+            for (int i = 0; i < Group::kWaves; ++i) keys[i] = maxima[threadIdx.x + 64 * i];
             const uint32_t key = reached(keys, a.top);
             if (threadIdx.x == 0) bound = key ? unordered(key << 16) : kLowest;
         }
@@ -389,7 +392,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
 #pragma unroll
             for (int k = 1; k < K; ++k) one = which == k ? raw[k] : one;
             C::widen(one, v);
-            const int at = chunk_at<VEC>(begin + lane + which * Group::kSize, nq, a.classes);
+            const int at = chunk_at<VEC>(begin + lane + which * TEAM, nq, a.classes);
             int hits = 0;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) hits += v[i] >= least;
@@ -403,14 +406,14 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
         }
         Group::sync();
         int n = *count;
-        if (n > kEntries) n = select_exactly<BF16, VEC, WAVE>(x, begin, end, nq, a.classes, a.top, least, list, count, meet[0]);
+        if (n > kEntries) n = select_exactly<BF16, VEC, TEAM>(x, begin, end, nq, a.classes, a.top, least, list, count, meet[0]);
         auto leave = [&](int rank, uint64_t entry) {
             if (alone) write_entry(a, row, rank, entry, p, log2_S);
             else lists[int64_t(unit) * a.top + rank] = entry;
         };
         if (!WAVE && n <= 128) {
             // several threads an entry, each against a part of the others
-            const int across = n <= 64 ? 64 : 128, each = (n * across + kThreads - 1) / kThreads, i = threadIdx.x % across, first = threadIdx.x / across * each;
+            const int across = n <= 64 ? 64 : 128, each = (n * across + TEAM - 1) / TEAM, i = threadIdx.x % across, first = threadIdx.x / across * each;
             if (threadIdx.x < across) ranks[threadIdx.x] = 0;
             __syncthreads();
             uint64_t entry = 0;
@@ -424,7 +427,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
             __syncthreads();
             if (threadIdx.x < n && ranks[i] < a.top) leave(ranks[i], entry);
         } else {
-            for (int i = lane; i < n; i += Group::kSize) {
+            for (int i = lane; i < n; i += TEAM) {
                 const uint64_t entry = list[i];
                 int rank = 0;
 #pragma unroll 8
@@ -432,7 +435,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
                 if (rank < a.top) leave(rank, entry);
             }
         }
-        for (int rank = n + lane; rank < a.top; rank += Group::kSize) leave(rank, 0);
+        for (int rank = n + lane; rank < a.top; rank += TEAM) leave(rank, 0);
     }
 }
 
@@ -553,7 +556,7 @@ LogProbsPlan plan_log_probs(int64_t rows, int64_t classes, bool bf16, int top)
     p.vec = classes < (bf16 ? 8 : 4) ? 1 : bf16 ? 8 : 4;
     p.chunks = static_cast<int>((classes + p.vec - 1) / p.vec);
     p.wave = p.chunks <= 64 * 8;
-    const int threads = p.wave ? 64 : kThreads;
+    const int threads = p.wave ? 64 : kTeam;
     p.slices = p.wave ? 1 : (p.chunks + threads * 8 - 1) / (threads * 8);
     p.slice = (p.chunks + p.slices - 1) / p.slices;
     p.slices = (p.chunks + p.slice - 1) / p.slice;
@@ -563,10 +566,10 @@ LogProbsPlan plan_log_probs(int64_t rows, int64_t classes, bool bf16, int top)
     return p;
 }
 
-template <bool BF16, int VEC, int K, bool WAVE> void launch_slices(const LogProbsArgs &a, const LogProbsPlan &p, Part *parts, uint64_t *lists, hipStream_t stream)
+template <bool BF16, int VEC, int K, int TEAM> void launch_slices(const LogProbsArgs &a, const LogProbsPlan &p, Part *parts, uint64_t *lists, hipStream_t stream)
 {
-    const unsigned groups = static_cast<unsigned>(WAVE ? (a.rows + 3) / 4 : a.rows * p.slices);
-    (a.top ? log_probs_slices_kernel<BF16, VEC, K, WAVE, true> : log_probs_slices_kernel<BF16, VEC, K, WAVE, false>)<<<groups, kThreads, 0, stream>>>(a, p.slice, p.slices, parts,
+    const unsigned groups = static_cast<unsigned>(TEAM == 64 ? (a.rows + 3) / 4 : a.rows * p.slices);
+    (a.top ? log_probs_slices_kernel<BF16, VEC, K, TEAM, true> : log_probs_slices_kernel<BF16, VEC, K, TEAM, false>)<<<groups, TEAM == 64 ? kThreads : TEAM, 0, stream>>>(a, p.slice, p.slices, parts,
                                                                                                                                                    lists);
 }
 
@@ -586,12 +589,12 @@ template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan
         if (b.top_logp) b.top_logp += row * a.top;
         if (b.largest) b.largest += row;
         if (b.log_sum) b.log_sum += row;
-        if (p.vec == 1) launch_slices<BF16, 1, 1, true>(b, p, parts, lists, stream);
-        else if (!p.wave) launch_slices<BF16, VEC, 8, false>(b, p, parts, lists, stream);
-        else if (p.k == 1) launch_slices<BF16, VEC, 1, true>(b, p, parts, lists, stream);
-        else if (p.k == 2) launch_slices<BF16, VEC, 2, true>(b, p, parts, lists, stream);
-        else if (p.k == 4) launch_slices<BF16, VEC, 4, true>(b, p, parts, lists, stream);
-        else launch_slices<BF16, VEC, 8, true>(b, p, parts, lists, stream);
+        if (p.vec == 1) launch_slices<BF16, 1, 1, 64>(b, p, parts, lists, stream);
+        else if (!p.wave) launch_slices<BF16, VEC, 8, kTeam>(b, p, parts, lists, stream);
+        else if (p.k == 1) launch_slices<BF16, VEC, 1, 64>(b, p, parts, lists, stream);
+        else if (p.k == 2) launch_slices<BF16, VEC, 2, 64>(b, p, parts, lists, stream);
+        else if (p.k == 4) launch_slices<BF16, VEC, 4, 64>(b, p, parts, lists, stream);
+        else launch_slices<BF16, VEC, 8, 64>(b, p, parts, lists, stream);
         if (p.slices > 1) {
             const unsigned groups = static_cast<unsigned>(b.rows);
             const size_t lds = (kListsAtOnce + 2) * size_t(a.top) * 8;

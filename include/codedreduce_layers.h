@@ -154,7 +154,7 @@ int cr_softmax_loss(int64_t rows, int64_t classes, int dtype, const void *logits
  *   shape         of dy, dtype that of dy;   bounds, runs  as above
  *   dtable        runs x vocabulary x channels floats
  * cr_embedding_workspace_bytes: what the gradient needs (256-byte aligned): 16 bytes a position (17 of more than one run), two rows of floats for
- * each piece (16 to 256 positions), a bit for each row of up to 128 runs. */
+ * each piece (16 to 256 positions), a byte for each row of up to 128 runs. */
 int cr_embedding_workspace_bytes(const cr_layer_shape_t *shape, int64_t vocabulary, const int64_t *bounds, int runs, size_t *backward_bytes);
 int cr_embedding_forward(const cr_layer_shape_t *shape, const cr_layer_view_t *tokens, const void *table, int table_dtype, int64_t vocabulary,
                          float scale, const cr_layer_view_t *y, void *hip_stream);

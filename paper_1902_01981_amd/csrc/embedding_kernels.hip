@@ -7,8 +7,8 @@
 //   sort_few_kernel            a stable sort of the positions by token, nine bits of it or fewer a pass, by one workgroup;
 //   sort_count_kernel, sort_place_kernel   by many, a pair of launches a pass
 //   embedding_sums_kernel, embedding_wide_sums_kernel   pieces of the sorted positions: sums of a cell (a run's token) that lies in a piece go to the
-//                              gradient, others to the workspace
-//   embedding_rest_kernel      cells of several pieces, and the rows of the gradient that no position has
+//                              gradient, others to the workspace; rows of the gradient that no position has are cleared beside them
+//   embedding_join_kernel      cells of several pieces
 #include "layers_device.h"
 
 #include <algorithm>
@@ -17,7 +17,7 @@ namespace cr {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kThreads = 256;
 
 // n / d for n < 2^31, by a product
 struct Divisor {
@@ -125,11 +125,46 @@ template <bool BF16, bool TABLE_BF16> void launch_forward(const EmbeddingArgs &a
     (C < VEC ? embedding_forward_kernel<BF16, TABLE_BF16, 1> : embedding_forward_kernel<BF16, TABLE_BF16, VEC>)<<<grid, kThreads, 0, stream>>>(a, tokens, out, Divisor(nq), chunks);
 }
 
+// ---- rows of zeros ---------------------------------------------------------------------------------------------------------------
+// Rows without positions, `neighbours` at a time; met: a byte for each row, 1 where it has positions; null: all rows are cleared.
+struct Zeros {
+    float *dtable;
+    int channels, vocabulary, runs, neighbours, parts;   // parts: workgroups that share such rows
+    const uint8_t *met;
+    int64_t workgroups;
+};
+__device__ __forceinline__ void clear_rows(const Zeros &z, int64_t workgroup)
+{
+    const f4 none = {0.f, 0.f, 0.f, 0.f};
+    const int part = static_cast<int>(workgroup % z.parts);
+    const int64_t groups = (z.vocabulary + z.neighbours - 1) / z.neighbours, all = groups * z.runs, others = z.workgroups / z.parts;
+    for (int64_t i = workgroup / z.parts; i < all; i += others) {
+        const int64_t run = i / groups;
+        const int first = static_cast<int>(i - run * groups) * z.neighbours, count = min(z.neighbours, z.vocabulary - first);
+        float *rows = z.dtable + (run * z.vocabulary + first) * z.channels;
+        uint64_t have = 0;
+        if (z.met) {
+            const int lane = threadIdx.x % 64;
+            have = __ballot(lane < count && z.met[run * z.vocabulary + first + min(lane, count - 1)]);
+        }
+        auto clear = [&](float *from, int64_t floats) {
+            const int64_t whole = floats / 4;
+            for (int64_t c = int64_t(part) * static_cast<int>(blockDim.x) + threadIdx.x; c < whole; c += int64_t(z.parts) * static_cast<int>(blockDim.x)) Chunk<false, 4>::store(from + 4 * c, none);
+            if (part == 0 && threadIdx.x < floats - 4 * whole) from[4 * whole + threadIdx.x] = 0.f;
+        };
+        if (have == 0) {
+            clear(rows, int64_t(count) * z.channels);
+        } else {
+            for (int r = 0; r < count; ++r)
+                if (!(have >> r & 1)) clear(rows + int64_t(r) * z.channels, z.channels);
+        }
+    }
+}
 // ---- the sort --------------------------------------------------------------------------------------------------------------------
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kKeysOfLane = 8;
-constexpr int kTile = kSortThreads * kKeysOfLane;        // positions that a workgroup sorts at once: a stretch of 512 per wavefront
+constexpr int kMostTile = kSortThreads * kKeysOfLane;    // positions that a workgroup sorts at once, a stretch of them per wavefront
 constexpr int kDigits = 512;                             // of a pass, at most
-constexpr int kMostBlocks = 256;                         // of a pass, each with as many tiles as it takes
+constexpr int kMostBlocks = 128;                         // of a pass, each with as many tiles as it takes: every one adds up the digits of all
 
 // Runs of a batch, by the first of their points in it.
 struct BatchRuns {
@@ -157,7 +192,10 @@ struct SortPass {
     uint8_t *run_out;                                    // of the last pass, if there are several runs
     uint32_t *counts;                                    // [workgroup][digit]
     uint32_t n;                                          // positions
-    int tiles, bits, shift;                              // tiles of a workgroup; bits of a digit
+    int tiles, steps, bits, shift;                       // tiles of a workgroup; steps of a wavefront in a tile; bits of a digit
+    uint8_t *met;                                        // cleared and written by the first pass: see Zeros
+    int64_t cells;
+    __device__ __forceinline__ int tile() const { return steps * kSortThreads; }
     __device__ __forceinline__ uint32_t key(uint32_t i) const
     {
         if (!tokens) return keys[i];
@@ -202,13 +240,14 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t mine, uint32_t *sums)
     return before;
 }
 
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortPass s, uint64_t *bits, int64_t words)
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortPass s)
 {
     __shared__ uint32_t count[kDigits];
-    for (int64_t w = int64_t(blockIdx.x) * kSortThreads + threadIdx.x; w < words; w += int64_t(gridDim.x) * kSortThreads) bits[w] = 0;
+    if (s.tokens)
+        for (int64_t c = int64_t(blockIdx.x) * kSortThreads + threadIdx.x; c < s.cells; c += int64_t(gridDim.x) * kSortThreads) s.met[c] = 0;
     if (threadIdx.x < kDigits) count[threadIdx.x] = 0;
     __syncthreads();
-    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * kTile, end = std::min<uint64_t>(begin + uint64_t(s.tiles) * kTile, s.n);
+    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * s.tile(), end = std::min<uint64_t>(begin + uint64_t(s.tiles) * s.tile(), s.n);
     for (uint64_t i = begin + threadIdx.x; i < end; i += kSortThreads) atomicAdd(&count[s.key(static_cast<uint32_t>(i)) >> s.shift & ((1u << s.bits) - 1)], 1u);
     __syncthreads();
     if (threadIdx.x < kDigits) s.counts[blockIdx.x * kDigits + threadIdx.x] = count[threadIdx.x];
@@ -244,23 +283,27 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(SortPass s, Ba
     }
     uint32_t next = before + digits_before(total, sums); // the place of the next key with this thread's digit, in the first kDigits threads
 
-    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * kTile;
+    const uint64_t begin = uint64_t(blockIdx.x) * s.tiles * s.tile();
     for (int tile = 0; tile < s.tiles; ++tile) {
-        const uint64_t first = begin + uint64_t(tile) * kTile;
+        const uint64_t first = begin + uint64_t(tile) * s.tile();
         if (first >= s.n) break;
         __syncthreads();
         for (int w = half; w < kSortWaves; w += 2) place[w][digit] = 0;
         __syncthreads();
         uint32_t key[kKeysOfLane], order[kKeysOfLane], rank[kKeysOfLane];
-        const uint64_t own = first + wave * (kTile / kSortWaves) + lane;
+        const uint64_t own = first + wave * s.steps * 64 + lane, end = std::min<uint64_t>(s.n, first + (wave + 1) * s.steps * 64);
 #pragma unroll
         for (int u = 0; u < kKeysOfLane; ++u) {
+            if (u >= s.steps) break;
             const uint32_t j = static_cast<uint32_t>(std::min<uint64_t>(own + u * 64, s.n - 1));
             key[u] = s.key(j);
             order[u] = s.tokens ? j : s.order[j];
         }
 #pragma unroll
-        for (int u = 0; u < kKeysOfLane; ++u) rank[u] = rank_of(key[u] >> s.shift & mask, s.bits, own + u * 64 < s.n, place[wave]);
+        for (int u = 0; u < kKeysOfLane; ++u) {
+            if (u >= s.steps) break;
+            rank[u] = rank_of(key[u] >> s.shift & mask, s.bits, own + u * 64 < end, place[wave]);
+        }
         __syncthreads();
         if (!half)
             for (int w = 0; w < kSortWaves; ++w) {
@@ -271,31 +314,45 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_kernel(SortPass s, Ba
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kKeysOfLane; ++u)
-            if (own + u * 64 < s.n) s.put(runs, place[wave][key[u] >> s.shift & mask] + rank[u], key[u], order[u]);
+            if (own + u * 64 < end) {
+                s.put(runs, place[wave][key[u] >> s.shift & mask] + rank[u], key[u], order[u]);
+                if (s.tokens && key[u] < s.vocabulary) {
+                    const int64_t run = runs.runs > 1 ? runs.of(static_cast<int>(s.walk.positions.of(order[u]))) : 0;
+                    s.met[run * s.vocabulary + key[u]] = 1;
+                }
+            }
     }
 }
 
-// Positions that one workgroup holds: all passes in one launch.
-__global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortPass s, BatchRuns runs, int passes, uint64_t *bits, int64_t words)
+// Positions that one workgroup holds: all passes in one launch.  The others clear the whole gradient meanwhile: rows that positions have are written twice,
+// 8 192 of them at most.
+__global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortPass s, BatchRuns runs, int passes, Zeros z)
 {
-    __shared__ uint32_t place[kSortWaves][kDigits], sums[kDigits / 64], keys[kTile];
-    __shared__ uint16_t orders[kTile];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, own = wave * (kTile / kSortWaves) + lane, n = static_cast<int>(s.n);
+    __shared__ uint32_t place[kSortWaves][kDigits], sums[kDigits / 64], keys[kMostTile];
+    __shared__ uint16_t orders[kMostTile];
+    if (blockIdx.x > 0) {
+        clear_rows(z, blockIdx.x - 1);
+        return;
+    }
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = static_cast<int>(s.n), steps = (n + kSortThreads - 1) / kSortThreads;
+    const int own = wave * steps * 64 + lane, end = std::min(n, (wave + 1) * steps * 64);
     const uint32_t mask = (1u << s.bits) - 1;
-    for (int64_t w = threadIdx.x; w < words; w += kSortThreads) bits[w] = 0;
     uint32_t key[kKeysOfLane], rank[kKeysOfLane];
     int order[kKeysOfLane];
 #pragma unroll
     for (int u = 0; u < kKeysOfLane; ++u) {
         order[u] = own + u * 64;
-        key[u] = s.key(std::min(own + u * 64, n - 1));
+        key[u] = u < steps ? s.key(std::min(own + u * 64, n - 1)) : 0;
     }
     for (int pass = 0; pass < passes; ++pass) {
         const int shift = pass * s.bits;
         for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) place[i / kDigits][i % kDigits] = 0;
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < kKeysOfLane; ++u) rank[u] = rank_of(key[u] >> shift & mask, s.bits, own + u * 64 < n, place[wave]);
+        for (int u = 0; u < kKeysOfLane; ++u) {
+            if (u >= steps) break;
+            rank[u] = rank_of(key[u] >> shift & mask, s.bits, own + u * 64 < end, place[wave]);
+        }
         __syncthreads();
         uint32_t total = 0;
         if (threadIdx.x < kDigits)
@@ -310,7 +367,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortPass s, Batc
         __syncthreads();
 #pragma unroll
         for (int u = 0; u < kKeysOfLane; ++u)
-            if (own + u * 64 < n) {
+            if (own + u * 64 < end) {
                 const uint32_t to = place[wave][key[u] >> shift & mask] + rank[u];
                 keys[to] = key[u];
                 orders[to] = static_cast<uint16_t>(order[u]);
@@ -325,7 +382,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_few_kernel(SortPass s, Batc
     }
 #pragma unroll
     for (int u = 0; u < kKeysOfLane; ++u)
-        if (own + u * 64 < n) s.put(runs, own + u * 64, key[u], order[u]);
+        if (own + u * 64 < end) s.put(runs, own + u * 64, key[u], order[u]);
 }
 
 // ---- the sums --------------------------------------------------------------------------------------------------------------------
@@ -349,20 +406,22 @@ struct Gradient {
     int channels;
     float scale;
     float *dtable, *parts;                               // parts: two rows a piece, what began before it and what goes on behind it
-    uint64_t *bits;                                      // a bit for each cell that has positions
-    int64_t words;                                       // of a run
 };
 
 constexpr int kRowsAtOnce = 8;
 template <int VEC> __device__ __forceinline__ int chunk_of(int q, int nq, int channels) { return q < nq - 1 ? q * VEC : channels - VEC; }
 
 // TS lanes per piece, each with a chunk of the channels, for rows of up to 32 chunks.
-template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads) embedding_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs)
+template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads) embedding_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs, unsigned workgroups, Zeros z)
 {
+    if (blockIdx.x >= workgroups) {                      // rows that no position has, behind the sums: there is room in their gaps
+        clear_rows(z, blockIdx.x - workgroups);
+        return;
+    }
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
     const uint64_t teams = uint64_t(s.pieces) * slabs;
-    for (uint64_t team = uint64_t(blockIdx.x) * (kThreads / TS) + threadIdx.x / TS; team < teams; team += uint64_t(gridDim.x) * (kThreads / TS)) {
+    for (uint64_t team = uint64_t(blockIdx.x) * (kThreads / TS) + threadIdx.x / TS; team < teams; team += uint64_t(workgroups) * (kThreads / TS)) {
         const unsigned piece = static_cast<unsigned>(team / slabs);
         const int q = static_cast<int>(team % slabs) * TS + threadIdx.x % TS;
         if (q >= nq) continue;
@@ -377,7 +436,6 @@ template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads
         for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
         auto leave = [&](bool ends) {
             if (now.key >= s.vocabulary) return;
-            if (begun && q == 0) atomicOr(reinterpret_cast<unsigned long long *>(g.bits + now.run * g.words + now.key / 64), 1ull << now.key % 64);
             float *to;
             float by = 1.f;
             if (begun && ends) {
@@ -423,13 +481,17 @@ template <bool BF16, int VEC, int TS> __global__ void __launch_bounds__(kThreads
 
 // Wider rows: a wavefront per piece and 64 chunks.  Its lanes look up 64 positions at once, what is at them is a scalar then; a row's place in the registers
 // takes the row eight further on as soon as it is added.
-template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedding_wide_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs)
+template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedding_wide_sums_kernel(Gradient g, Sorted s, int nq, unsigned slabs, unsigned workgroups, Zeros z)
 {
+    if (blockIdx.x >= workgroups) {                      // rows that no position has, behind the sums: there is room in their gaps
+        clear_rows(z, blockIdx.x - workgroups);
+        return;
+    }
     using C = Chunk<BF16, VEC>;
     using T = typename C::element;
     const int lane = threadIdx.x % 64;
     const uint64_t teams = uint64_t(s.pieces) * slabs;
-    for (uint64_t team = uint64_t(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); team < teams; team += uint64_t(gridDim.x) * (kThreads / 64)) {
+    for (uint64_t team = uint64_t(blockIdx.x) * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64); team < teams; team += uint64_t(workgroups) * (kThreads / 64)) {
         const unsigned piece = static_cast<unsigned>(team / slabs);
         const int q = static_cast<int>(team % slabs) * 64 + lane;
         const uint32_t begin = piece * s.length, end = min(begin + s.length, s.n);
@@ -460,7 +522,6 @@ template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedd
         for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
         auto leave = [&](bool ends) {
             if (now.key >= s.vocabulary) return;
-            if (begun && q == 0) atomicOr(reinterpret_cast<unsigned long long *>(g.bits + now.run * g.words + now.key / 64), 1ull << now.key % 64);
             const bool whole = begun && ends;
             float *to = whole ? g.dtable + (int64_t(now.run) * s.vocabulary + now.key) * g.channels : g.parts + (2 * int64_t(piece) + begun) * g.channels;
             const float by = whole ? g.scale : 1.f;
@@ -505,92 +566,74 @@ template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedd
     }
 }
 
-// The cell that begins in a piece and goes on behind it: its parts, added up in 64 bits.
-__device__ __forceinline__ void join_cell(const Gradient &g, const Sorted &s, unsigned piece, int part, int parts)
+// The cell that begins in a piece and goes on behind it: its parts, added up in 64 bits.  A thread has two chunks of VEC channels; what threads a workgroup has
+// beside those across a part's channels (512 at most) share the pieces out.
+template <int VEC> __global__ void __launch_bounds__(kThreads) embedding_join_kernel(Gradient g, Sorted s, int nq, int across, int parts)
 {
-    __shared__ double meet[kWaves][64 * 4];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const uint32_t begin = piece * s.length, end = min(begin + s.length, s.n);
-    if (end == s.n) return;
-    const Cell now = cell_at(s, end - 1);
-    if (now.key >= s.vocabulary || !(cell_at(s, end) == now)) return;
-    if (begin > 0 && cell_at(s, begin - 1) == now) return;           // it began before
-    unsigned more = 0;                                   // pieces behind this one that the cell reaches into
-    for (;;) {
-        const unsigned i = piece + 1 + more + threadIdx.x;
-        const int count = __syncthreads_count(i < s.pieces && cell_at(s, i * s.length) == now);
-        more += count;
-        if (count < kThreads) break;
-    }
-    for (int64_t c0 = int64_t(part) * 256; c0 < g.channels; c0 += int64_t(parts) * 256) {
-        double sum[4] = {};
-        constexpr int U = 4;
-        for (unsigned p = wave; p <= more; p += U * kWaves) {
-            float v[U][4];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const unsigned pu = min(p + u * kWaves, more);
-                const float *row = g.parts + (2 * int64_t(piece + pu) + (pu == 0)) * g.channels;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) v[u][i] = row[std::min<int64_t>(c0 + i * 64 + lane, g.channels - 1)];
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[i] += p + u * kWaves <= more ? v[u][i] : 0.f;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) meet[wave][i * 64 + lane] = sum[i];
-        __syncthreads();
-        double total = 0.0;
-        for (int w = 0; w < kWaves; ++w) total += meet[w][threadIdx.x];
-        const int64_t c = c0 + threadIdx.x;
-        if (c < g.channels) g.dtable[(int64_t(now.run) * s.vocabulary + now.key) * g.channels + c] = static_cast<float>(total) * g.scale;
-        __syncthreads();
-    }
-}
-
-// Rows without positions, `neighbours` at a time; bits null: all rows.
-struct Zeros {
-    float *dtable;
-    int channels, vocabulary, runs, neighbours, parts;   // parts: workgroups that share such rows
-    const uint64_t *bits;
-    int64_t words, workgroups;
-};
-__device__ __forceinline__ void clear_rows(const Zeros &z, int64_t workgroup)
-{
-    const f4 none = {0.f, 0.f, 0.f, 0.f};
-    const int part = static_cast<int>(workgroup % z.parts);
-    const int64_t groups = (z.vocabulary + z.neighbours - 1) / z.neighbours, all = groups * z.runs, others = z.workgroups / z.parts;
-    for (int64_t i = workgroup / z.parts; i < all; i += others) {
-        const int64_t run = i / groups;
-        const int first = static_cast<int>(i - run * groups) * z.neighbours, count = min(z.neighbours, z.vocabulary - first);
-        float *rows = z.dtable + (run * z.vocabulary + first) * z.channels;
-        uint64_t have = z.bits ? z.bits[run * z.words + first / 64] >> first % 64 : 0;
-        if (count < 64) have &= (uint64_t(1) << count) - 1;
-        auto clear = [&](float *from, int64_t floats) {
-            const int64_t whole = floats / 4;
-            for (int64_t c = int64_t(part) * kThreads + threadIdx.x; c < whole; c += int64_t(z.parts) * kThreads) Chunk<false, 4>::store(from + 4 * c, none);
-            if (part == 0 && threadIdx.x < floats - 4 * whole) from[4 * whole + threadIdx.x] = 0.f;
-        };
-        if (have == 0) {
-            clear(rows, int64_t(count) * z.channels);
-        } else {
-            for (int r = 0; r < count; ++r)
-                if (!(have >> r & 1)) clear(rows + int64_t(r) * z.channels, z.channels);
-        }
-    }
-}
-// What is left once the sums are there: cells of several pieces, and rows of none.  The two share no row.
-__global__ void __launch_bounds__(kThreads) embedding_rest_kernel(Gradient g, Sorted s, Zeros z, unsigned joins, int parts)
-{
-    if (blockIdx.x >= joins) {
-        clear_rows(z, blockIdx.x - joins);
-        return;
-    }
+    constexpr int J = 2, U = 4;
+    __shared__ double meet[J][VEC][kThreads];
     const int64_t all = int64_t(s.pieces) * parts;
-    for (int64_t i = blockIdx.x; i < all; i += joins) join_cell(g, s, static_cast<unsigned>(i / parts), static_cast<int>(i % parts), parts);
+    const int team = threadIdx.x / across, teams = kThreads / across, lane = threadIdx.x % across;
+    for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+        const unsigned piece = static_cast<unsigned>(i / parts);
+        const uint32_t begin = piece * s.length, end = min(begin + s.length, s.n);
+        const Cell before = cell_at(s, max(begin, 1u) - 1), now = cell_at(s, end - 1), behind = cell_at(s, min(end, s.n - 1));
+        if (end == s.n || now.key >= s.vocabulary || !(behind == now) || (begin > 0 && before == now)) continue;
+        unsigned more = 0;                               // pieces behind this one that the cell reaches into
+        for (;;) {
+            const unsigned p = piece + 1 + more + threadIdx.x;
+            const int count = __syncthreads_count(p < s.pieces && cell_at(s, std::min(p, s.pieces - 1) * s.length) == now);
+            more += count;
+            if (count < kThreads) break;
+        }
+        for (int q0 = static_cast<int>(i % parts) * J * across; q0 < nq; q0 += parts * J * across) {
+            double sum[J][VEC] = {};
+            int at[J];
+#pragma unroll
+            for (int j = 0; j < J; ++j) at[j] = chunk_of<VEC>(min(q0 + j * across + lane, nq - 1), nq, g.channels);
+            for (unsigned p = team; p <= more; p += U * teams) {
+                typename Chunk<false, VEC>::raw raw[U][J];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const unsigned pu = min(p + u * teams, more);
+                    const float *row = g.parts + (2 * int64_t(piece + pu) + (pu == 0)) * g.channels;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) raw[u][j] = Chunk<false, VEC>::load(row + at[j]);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    if (p + u * teams > more) break;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+                        float v[VEC];
+                        Chunk<false, VEC>::widen(raw[u][j], v);
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) sum[j][c] += v[c];
+                    }
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+#pragma unroll
+                for (int c = 0; c < VEC; ++c) meet[j][c][threadIdx.x] = sum[j][c];
+            }
+            __syncthreads();
+            if (team == 0) {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    float v[VEC];
+#pragma unroll
+                    for (int c = 0; c < VEC; ++c) {
+                        double total = 0.0;
+                        for (int t = 0; t < teams; ++t) total += meet[j][c][t * across + lane];
+                        v[c] = static_cast<float>(total) * g.scale;
+                    }
+                    if (q0 + j * across + lane < nq) store_row<false, VEC>(g.dtable, (int64_t(now.run) * s.vocabulary + now.key) * g.channels + at[j], v);
+                }
+            }
+            __syncthreads();
+        }
+    }
 }
 
 // ---- what a gradient needs -------------------------------------------------------------------------------------------------------
@@ -599,16 +642,18 @@ struct GradPlan {
     int passes, digit_bits;      // of the sort; of a digit of it
     int vec, nq, team;           // channels of a chunk, chunks of a row, lanes of a piece
     unsigned slabs;
-    int64_t words;               // of bits, per run
-    size_t keys[2], order[2], run, counts, parts, bits, bytes;       // offsets
+    size_t keys[2], order[2], run, counts, parts, met, bytes;        // offsets
 };
-unsigned blocks_of(uint32_t n) { return std::min<unsigned>((uint64_t(n) + kTile - 1) / kTile, kMostBlocks); }
-// Pieces that give some 8 192 wavefronts, of 16 to 256 positions.
+// Workgroups of the sort: one where it holds all positions, else so many that a tile of each is as small as their number allows.
+unsigned blocks_of(uint32_t n) { return n <= kMostTile ? 1 : static_cast<unsigned>(std::min<int64_t>((int64_t(n) + kSortThreads - 1) / kSortThreads, kMostBlocks)); }
+// Pieces of 16 to 256 positions that fill the chip a whole number of times, once if they can: 983 040 rows of 1 KB in pieces of 128, which left 7 % of the
+// wavefronts for a second time, took 287 us.
 int piece_length(uint32_t n, int team, unsigned slabs)
 {
-    int length = 16;
-    while (length < 256 && uint64_t(n) * slabs * team / 64 > uint64_t(length) * 8192) length *= 2;
-    return length;
+    constexpr int64_t kWavefronts = 256 * 28;            // compute units, and what their registers take at once
+    const int64_t work = (int64_t(n) * slabs * team + 63) / 64, times = std::max<int64_t>(1, (work + 256 * kWavefronts - 1) / (256 * kWavefronts));
+    const int64_t length = (work + times * kWavefronts - 1) / (times * kWavefronts);
+    return static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(team < 64 ? 64 : 16, (length + 7) / 8 * 8)));
 }
 
 GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *bounds, int runs, uint32_t n)
@@ -624,7 +669,6 @@ GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *b
     p.nq = (shape.channels + p.vec - 1) / p.vec;
     for (p.team = 1; p.team < 64 && p.team < p.nq;) p.team *= 2;
     p.slabs = (p.nq + p.team - 1) / p.team;
-    p.words = (int64_t(vocabulary) + 63) / 64;
     const int length = piece_length(n, p.team, p.slabs);
     const uint64_t pieces = (uint64_t(n) + length - 1) / length;
     size_t at = 0;
@@ -640,7 +684,7 @@ GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *b
     p.run = take(runs > 1 ? n : 0);
     p.counts = take(size_t(blocks_of(n)) * kDigits * 4);
     p.parts = take(pieces * 2 * shape.channels * 4);
-    p.bits = take(size_t(std::min(runs, BatchRuns::kRuns)) * p.words * 8);
+    p.met = take(size_t(std::min(runs, BatchRuns::kRuns)) * vocabulary);
     p.bytes = at;
     return p;
 }
@@ -651,11 +695,12 @@ uint32_t most_positions(const LayerShape &shape, const int64_t *bounds, int runs
     return static_cast<uint32_t>(most * shape.positions);
 }
 
-template <bool BF16, int VEC> void launch_sums(const Gradient &g, const Sorted &s, const GradPlan &p, hipStream_t stream)
+template <bool BF16, int VEC> void launch_sums(const Gradient &g, const Sorted &s, const GradPlan &p, const Zeros &z, hipStream_t stream)
 {
     auto go = [&](auto kernel, int team) {
         const uint64_t teams = uint64_t(s.pieces) * p.slabs, per_block = kThreads / team;
-        kernel<<<static_cast<unsigned>(std::min<uint64_t>((teams + per_block - 1) / per_block, 1 << 20)), kThreads, 0, stream>>>(g, s, p.nq, p.slabs);
+        const unsigned workgroups = static_cast<unsigned>(std::min<uint64_t>((teams + per_block - 1) / per_block, 1 << 20));
+        kernel<<<workgroups + static_cast<unsigned>(z.workgroups), kThreads, 0, stream>>>(g, s, p.nq, p.slabs, workgroups, z);
     };
     switch (p.team) {
     case 1: return go(embedding_sums_kernel<BF16, VEC, 1>, 1);
@@ -670,18 +715,17 @@ template <bool BF16, int VEC> void launch_sums(const Gradient &g, const Sorted &
     }
 }
 
-// cells: of several pieces may be among the positions
-void launch_rest(const EmbeddingGradArgs &a, const Gradient &g, const Sorted &s, int runs, bool cells, hipStream_t stream)
+Zeros plan_zeros(const EmbeddingGradArgs &a, float *dtable, int runs, const uint8_t *met, int64_t most_workgroups)
 {
-    Zeros z = {g.dtable, a.shape.channels, a.vocabulary, runs, 64, 1, g.bits, g.words, 0};
+    Zeros z = {dtable, a.shape.channels, a.vocabulary, runs, 64, 1, met, 0};
     while (z.neighbours > 1 && int64_t(z.neighbours) * z.channels > 16384) z.neighbours /= 2;          // at most 64 KB of a workgroup
     z.parts = std::max(1, std::min(1024, z.channels / 16384));
     const int64_t groups = (int64_t(a.vocabulary) + z.neighbours - 1) / z.neighbours * runs;
-    z.workgroups = std::min<int64_t>(groups, (1 << 20) / z.parts) * z.parts;
-    const int parts = std::min((a.shape.channels + 255) / 256, 64);
-    const unsigned joins = cells ? static_cast<unsigned>(std::min<int64_t>(int64_t(s.pieces) * parts, 1 << 22)) : 0;
-    embedding_rest_kernel<<<joins + static_cast<unsigned>(z.workgroups), kThreads, 0, stream>>>(g, s, z, joins, parts);
+    z.workgroups = std::min<int64_t>(groups, std::max<int64_t>(1, most_workgroups / z.parts)) * z.parts;
+    return z;
 }
+constexpr int64_t kFewZeros = 511;
+__global__ void __launch_bounds__(kThreads) embedding_zeros_kernel(Zeros z) { clear_rows(z, blockIdx.x); }
 
 }  // namespace
 
@@ -692,7 +736,7 @@ size_t embedding_backward_bytes(const LayerShape &shape, int vocabulary, const i
     size_t most = 0;                                     // pieces are shorter where there are fewer positions: every batch has to fit
     for (int r = 0; r < runs; r += BatchRuns::kRuns) {
         const int64_t points = bounds[std::min(runs, r + BatchRuns::kRuns)] - bounds[r];
-        most = std::max(most, plan_gradient(shape, vocabulary, bounds, runs, static_cast<uint32_t>(points * shape.positions)).bytes);
+        if (points > 0) most = std::max(most, plan_gradient(shape, vocabulary, bounds, runs, static_cast<uint32_t>(points * shape.positions)).bytes);
     }
     return most;
 }
@@ -716,27 +760,31 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
         float *dtable = a.dtable + int64_t(r0) * a.vocabulary * shape.channels;
         const uint32_t n = static_cast<uint32_t>((a.bounds[r0 + runs.runs] - first) * shape.positions);
         if (n == 0) {
-            const Gradient none = {nullptr, Walk(a.dy, shape.positions), shape.channels, a.scale, dtable, nullptr, nullptr, 0};
-            launch_rest(a, none, Sorted(), runs.runs, false, stream);
+            const Zeros z = plan_zeros(a, dtable, runs.runs, nullptr, 1 << 20);
+            embedding_zeros_kernel<<<static_cast<unsigned>(z.workgroups), kThreads, 0, stream>>>(z);
             continue;
         }
         const GradPlan p = plan_gradient(shape, a.vocabulary, a.bounds, a.runs, n);
         char *ws = static_cast<char *>(workspace);
         auto words = [&](size_t at) { return reinterpret_cast<uint32_t *>(ws + at); };
-        uint64_t *bits = reinterpret_cast<uint64_t *>(ws + p.bits);
+        uint8_t *met = reinterpret_cast<uint8_t *>(ws + p.met);
         const unsigned blocks = blocks_of(n);
-        const int tiles = static_cast<int>(((uint64_t(n) + kTile - 1) / kTile + blocks - 1) / blocks);
+        const int64_t own = (int64_t(n) + blocks - 1) / blocks;          // positions of a workgroup
+        const int steps = static_cast<int>(std::min<int64_t>(kKeysOfLane, (own + kSortThreads - 1) / kSortThreads));
+        const int tiles = static_cast<int>((own + steps * kSortThreads - 1) / (steps * kSortThreads));
         int end = 0;                                     // of the two buffers, the one that holds the sorted positions
         for (int pass = 0; pass < (blocks == 1 ? 1 : p.passes); ++pass) {
             const int to = pass % 2, from = 1 - to;
             const bool last = blocks == 1 || pass == p.passes - 1;
             const SortPass s = {pass == 0 ? static_cast<const int64_t *>(a.tokens.p) + first * a.tokens.point_stride : nullptr, Walk(a.tokens, shape.positions),
                                 static_cast<uint32_t>(a.vocabulary), words(p.keys[from]), words(p.order[from]), words(p.keys[to]), words(p.order[to]),
-                                last && a.runs > 1 ? reinterpret_cast<uint8_t *>(ws + p.run) : nullptr, words(p.counts), n, tiles, p.digit_bits, p.digit_bits * pass};
+                                last && a.runs > 1 ? reinterpret_cast<uint8_t *>(ws + p.run) : nullptr, words(p.counts), n, tiles, steps, p.digit_bits, p.digit_bits * pass, met,
+                                int64_t(runs.runs) * a.vocabulary};
             if (blocks == 1) {
-                sort_few_kernel<<<1, kSortThreads, 0, stream>>>(s, runs, p.passes, bits, p.words * runs.runs);
+                const Zeros z = plan_zeros(a, dtable, runs.runs, nullptr, kFewZeros);        // these stay
+                sort_few_kernel<<<1 + static_cast<unsigned>(z.workgroups), kSortThreads, 0, stream>>>(s, runs, p.passes, z);
             } else {
-                sort_count_kernel<<<blocks, kSortThreads, 0, stream>>>(s, bits, pass == 0 ? p.words * runs.runs : 0);
+                sort_count_kernel<<<blocks, kSortThreads, 0, stream>>>(s);
                 sort_place_kernel<<<blocks, kSortThreads, 0, stream>>>(s, runs);
             }
             end = to;
@@ -746,11 +794,20 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
                           static_cast<uint32_t>(a.vocabulary), length, static_cast<unsigned>((uint64_t(n) + length - 1) / length)};
         const size_t e = shape.bf16 ? 2 : 4;
         const Gradient g = {static_cast<const char *>(a.dy.p) + first * a.dy.point_stride * static_cast<int64_t>(e), Walk(a.dy, shape.positions), shape.channels, a.scale,
-                            dtable, reinterpret_cast<float *>(ws + p.parts), bits, p.words};
-        if (p.vec == 1) shape.bf16 ? launch_sums<true, 1>(g, s, p, stream) : launch_sums<false, 1>(g, s, p, stream);
-        else if (shape.bf16) launch_sums<true, 8>(g, s, p, stream);
-        else launch_sums<false, 4>(g, s, p, stream);
-        launch_rest(a, g, s, runs.runs, s.pieces > 1, stream);
+                            dtable, reinterpret_cast<float *>(ws + p.parts)};
+        Zeros z = {};
+        if (blocks > 1) z = plan_zeros(a, dtable, runs.runs, met, 1 << 20);
+        if (p.vec == 1) shape.bf16 ? launch_sums<true, 1>(g, s, p, z, stream) : launch_sums<false, 1>(g, s, p, z, stream);
+        else if (shape.bf16) launch_sums<true, 8>(g, s, p, z, stream);
+        else launch_sums<false, 4>(g, s, p, z, stream);
+        if (s.pieces > 1) {
+            const int vec = shape.channels < 4 ? 1 : 4, nq = (shape.channels + vec - 1) / vec;
+            int across = 2;
+            while (across < 64 && 2 * across < nq) across *= 2;
+            const int parts = std::min((nq + 2 * across - 1) / (2 * across), 64);
+            const unsigned groups = static_cast<unsigned>(std::min<int64_t>(int64_t(s.pieces) * parts, 1 << 22));
+            (vec == 1 ? embedding_join_kernel<1> : embedding_join_kernel<4>)<<<groups, kThreads, 0, stream>>>(g, s, nq, across, parts);
+        }
     }
     return hipGetLastError();
 }

@@ -104,8 +104,15 @@ def test_the_workspace_of_a_gradient():
         bounds = [points * r // runs for r in range(runs + 1)]
         status, need = _embedding_bytes(_shape(points, positions, channels, BF16), vocabulary, bounds, runs)
         n = points * positions
-        most = 17 * n + (n // 16 + 1) * 8 * channels + min(runs, 128) * (vocabulary // 8 + 8) + 512 * 1024 + 8 * 256
+        most = 17 * n + (n // 16 + 1) * 8 * channels + min(runs, 128) * vocabulary + 512 * 1024 + 8 * 256
         assert status == cr.CR_OK and 16 * (n // runs) <= need <= most
+
+
+def test_the_workspace_of_batches_of_runs_without_points():
+    """Runs are taken 128 at a time: a batch of them may have no points at all."""
+    for bounds in ([0] * 300 + [211], [0] + [211] * 300, [0] * 150 + [100] * 150 + [211]):
+        status, need = _embedding_bytes(_shape(211, 6, 20, BF16), 70, bounds, len(bounds) - 1)
+        assert status == cr.CR_OK and need >= 17 * 100 * 6
 
 
 def _scores(rows=3, classes=10, dtype=F32, logits=HERE, stride=10, tokens=HERE, logp=HERE, entropy=0, top=0, index=0, values=0, largest=0, log_sum=0, ws=0, nbytes=0):

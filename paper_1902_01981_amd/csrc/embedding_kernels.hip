@@ -43,7 +43,7 @@ struct Walk {
 };
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------------
-constexpr int kChunks = 4;       // of a thread
+constexpr int kChunks = 2;       // of a thread
 
 template <bool TABLE_BF16, int VEC> __device__ __forceinline__ void load_table(const void *table, int64_t at, float (&v)[VEC])
 {
@@ -64,18 +64,19 @@ template <bool TABLE_BF16, int VEC> __device__ __forceinline__ void load_table(c
         }
     }
 }
-template <bool BF16, int VEC> __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[VEC])
+// ONCE: past the caches
+template <bool BF16, int VEC, bool ONCE = false> __device__ __forceinline__ void store_row(void *y, int64_t at, const float (&v)[VEC])
 {
-    using T = typename Element<BF16>::type;
-    T *p = static_cast<T *>(y) + at;
-    if constexpr (VEC == 1) {
-        Element<BF16>::put(p, v[0]);
-    } else if constexpr (BF16) {
-        static_assert(VEC == 8);
-        Chunk<true, 8>::store(p, Chunk<true, 8>::narrow(v));
-    } else {
+    constexpr int kChunk = VEC == 1 ? 1 : BF16 ? 8 : 4;
+    using C = Chunk<BF16, kChunk>;
+    typename C::element *p = static_cast<typename C::element *>(y) + at;
 #pragma unroll
-        for (int h = 0; h < VEC / 4; ++h) Chunk<false, 4>::store(p + 4 * h, f4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]});
+    for (int h = 0; h < VEC / kChunk; ++h) {
+        float w[kChunk];
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) w[i] = v[h * kChunk + i];
+        if constexpr (ONCE) C::store_once(p + h * kChunk, C::narrow(w));
+        else C::store(p + h * kChunk, C::narrow(w));
     }
 }
 
@@ -110,7 +111,7 @@ __global__ void __launch_bounds__(kThreads) embedding_forward_kernel(EmbeddingAr
         for (int k = 0; k < kChunks; ++k) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) v[k][i] = token[k] < 0 ? 0.f : token[k] >= a.vocabulary ? __builtin_nanf("") : v[k][i] * a.scale;
-            store_row<BF16, VEC>(a.y.p, out.at(row[k]) + at[k], v[k]);
+            store_row<BF16, VEC, true>(a.y.p, out.at(row[k]) + at[k], v[k]);
         }
     }
 }
@@ -164,7 +165,7 @@ __device__ __forceinline__ void clear_rows(const Zeros &z, int64_t workgroup)
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kKeysOfLane = 8;
 constexpr int kMostTile = kSortThreads * kKeysOfLane;    // positions that a workgroup sorts at once, a stretch of them per wavefront
 constexpr int kDigits = 512;                             // of a pass, at most
-constexpr int kMostBlocks = 128;                         // of a pass, each with as many tiles as it takes: every one adds up the digits of all
+constexpr int kFewBlocks = 128, kMostBlocks = 256;       // of a pass: every one adds up the digits of all, so fewer where tiles are not full
 
 // Runs of a batch, by the first of their points in it.
 struct BatchRuns {
@@ -534,7 +535,7 @@ template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) embedd
         auto fetch = [&](int u, int of) {                // the row of position `of` of the 64 ahead
             const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(ahead.offset), of), hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(ahead.offset >> 32), of);
             const char *row = static_cast<const char *>(g.dy) + static_cast<int64_t>(uint64_t(hi) << 32 | lo) * static_cast<int64_t>(sizeof(T));
-            raw[u] = C::load(reinterpret_cast<const T *>(scalar(row) + lane_byte));
+            raw[u] = C::load_once(reinterpret_cast<const T *>(scalar(row) + lane_byte));
         };
 #pragma unroll
         for (int u = 0; u < kRowsAtOnce; ++u) fetch(u, u);
@@ -618,16 +619,22 @@ template <int VEC> __global__ void __launch_bounds__(kThreads) embedding_join_ke
                 for (int c = 0; c < VEC; ++c) meet[j][c][threadIdx.x] = sum[j][c];
             }
             __syncthreads();
+            for (int half = teams / 2; half > 0; half /= 2) {
+                if (team < half) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) {
+#pragma unroll
+                        for (int c = 0; c < VEC; ++c) meet[j][c][threadIdx.x] += meet[j][c][threadIdx.x + half * across];
+                    }
+                }
+                __syncthreads();
+            }
             if (team == 0) {
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     float v[VEC];
 #pragma unroll
-                    for (int c = 0; c < VEC; ++c) {
-                        double total = 0.0;
-                        for (int t = 0; t < teams; ++t) total += meet[j][c][t * across + lane];
-                        v[c] = static_cast<float>(total) * g.scale;
-                    }
+                    for (int c = 0; c < VEC; ++c) v[c] = static_cast<float>(meet[j][c][lane]) * g.scale;
                     if (q0 + j * across + lane < nq) store_row<false, VEC>(g.dtable, (int64_t(now.run) * s.vocabulary + now.key) * g.channels + at[j], v);
                 }
             }
@@ -645,7 +652,7 @@ struct GradPlan {
     size_t keys[2], order[2], run, counts, parts, met, bytes;        // offsets
 };
 // Workgroups of the sort: one where it holds all positions, else so many that a tile of each is as small as their number allows.
-unsigned blocks_of(uint32_t n) { return n <= kMostTile ? 1 : static_cast<unsigned>(std::min<int64_t>((int64_t(n) + kSortThreads - 1) / kSortThreads, kMostBlocks)); }
+unsigned blocks_of(uint32_t n) { return n <= kMostTile ? 1 : static_cast<unsigned>(std::min<int64_t>((int64_t(n) + kSortThreads - 1) / kSortThreads, n > kFewBlocks * kMostTile ? kMostBlocks : kFewBlocks)); }
 // Pieces of 16 to 256 positions that fill the chip a whole number of times, once if they can: 983 040 rows of 1 KB in pieces of 128, which left 7 % of the
 // wavefronts for a second time, took 287 us.
 int piece_length(uint32_t n, int team, unsigned slabs)

@@ -33,6 +33,7 @@ template <> struct Chunk<false, 1> {
     static __device__ __forceinline__ raw load(const element *p) { return *p; }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(p); }
     static __device__ __forceinline__ void store(element *p, raw r) { *p = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, p); }
     static __device__ __forceinline__ void widen(raw r, float (&v)[1]) { v[0] = r; }
     static __device__ __forceinline__ raw narrow(const float (&v)[1]) { return v[0]; }
 };
@@ -42,6 +43,7 @@ template <> struct Chunk<true, 1> {
     static __device__ __forceinline__ raw load(const element *p) { return *p; }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(p); }
     static __device__ __forceinline__ void store(element *p, raw r) { *p = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, p); }
     static __device__ __forceinline__ void widen(raw r, float (&v)[1]) { v[0] = __uint_as_float(static_cast<uint32_t>(r) << 16); }
     static __device__ __forceinline__ raw narrow(const float (&v)[1]) { return static_cast<raw>(pack_bf16(v[0], 0.f)); }
 };
@@ -52,6 +54,7 @@ template <> struct Chunk<false, 4> {
     static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
     static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[4]) { v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w; }
     static __device__ __forceinline__ raw narrow(const float (&v)[4]) { return raw{v[0], v[1], v[2], v[3]}; }
 };
@@ -62,6 +65,7 @@ template <> struct Chunk<true, 8> {
     static __device__ __forceinline__ raw load(const element *p) { return *reinterpret_cast<const memory *>(p); }
     static __device__ __forceinline__ raw load_once(const element *p) { return __builtin_nontemporal_load(reinterpret_cast<const memory *>(p)); }
     static __device__ __forceinline__ void store(element *p, raw r) { *reinterpret_cast<memory *>(p) = r; }
+    static __device__ __forceinline__ void store_once(element *p, raw r) { __builtin_nontemporal_store(r, reinterpret_cast<memory *>(p)); }
     static __device__ __forceinline__ void widen(const raw &r, float (&v)[8])
     {
         v[0] = __uint_as_float(r.x << 16); v[1] = __uint_as_float(r.x & 0xffff0000u);

@@ -261,6 +261,9 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
     __shared__ uint32_t maxima[WAVE || !TOP ? 1 : TEAM];
     __shared__ float bound;
     __shared__ int ranks[WAVE || !TOP ? 1 : 128];
+    constexpr int kHits = WAVE || !TOP ? 1 : 512;
+    __shared__ typename C::raw hit[kHits];
+    __shared__ int hit_at[kHits], hits;
     const int wave = threadIdx.x / 64, team = WAVE ? wave : 0, lane = threadIdx.x % TEAM;
     const int unit = WAVE ? blockIdx.x * kTeams + team : blockIdx.x;               // fewer than 2^22 in a batch
     const int row = WAVE || slices == 1 ? unit : unit / slices;
@@ -378,35 +381,63 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
             const uint32_t key = reached(keys, a.top);
             if (threadIdx.x == 0) bound = key ? unordered(key << 16) : kLowest;
         }
-        if (lane == 0) *count = 0;
+        if (lane == 0) {
+            *count = 0;
+            if constexpr (!WAVE) hits = 0;
+        }
         Group::sync();
         if constexpr (!WAVE) least = bound;
-        // the chunks with such elements, one of each lane at a time: few lanes have any, and fewer have several
-        unsigned chunks = 0;
+        bool all_kept = true;
+        if constexpr (WAVE) {
+            // the chunks with such elements, one of each lane at a time: few lanes have any, and fewer have several
+            unsigned chunks = 0;
 #pragma unroll
-        for (int k = 0; k < K; ++k) chunks |= most[k] >= least ? 1u << k : 0u;
-        while (chunks) {
-            const int which = __builtin_ctz(chunks);
-            chunks &= chunks - 1;
-            typename C::raw one = raw[0];
+            for (int k = 0; k < K; ++k) chunks |= most[k] >= least ? 1u << k : 0u;
+            while (chunks) {
+                const int which = __builtin_ctz(chunks);
+                chunks &= chunks - 1;
+                typename C::raw one = raw[0];
 #pragma unroll
-            for (int k = 1; k < K; ++k) one = which == k ? raw[k] : one;
-            C::widen(one, v);
-            const int at = chunk_at<VEC>(begin + lane + which * TEAM, nq, a.classes);
-            int hits = 0;
+                for (int k = 1; k < K; ++k) one = which == k ? raw[k] : one;
+                C::widen(one, v);
+                const int at = chunk_at<VEC>(begin + lane + which * TEAM, nq, a.classes);
+                int hits = 0;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) hits += v[i] >= least;
-            int to = atomicAdd(count, hits);
+                for (int i = 0; i < VEC; ++i) hits += v[i] >= least;
+                int to = atomicAdd(count, hits);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i)
-                if (v[i] >= least) {
-                    if (to < kEntries) list[to] = entry_of(v[i], at + i);
-                    ++to;
+                for (int i = 0; i < VEC; ++i)
+                    if (v[i] >= least) {
+                        if (to < kEntries) list[to] = entry_of(v[i], at + i);
+                        ++to;
+                    }
+            }
+        } else {
+            // the chunks with such elements to where all threads can look at them, an element each
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (most[k] >= least) {
+                    const int to = atomicAdd(&hits, 1);
+                    if (to < kHits) {
+                        hit[to] = raw[k];
+                        hit_at[to] = place(k);
+                    }
+                }
+            __syncthreads();
+            const int found = hits;
+            all_kept = found <= kHits;
+            if (all_kept)
+                for (int e = threadIdx.x; e < found * VEC; e += TEAM) {
+                    const float one = Element<BF16>::get(reinterpret_cast<const T *>(hit) + e);
+                    if (one >= least) {
+                        const int to = atomicAdd(count, 1);
+                        if (to < kEntries) list[to] = entry_of(one, hit_at[e / VEC] + e % VEC);
+                    }
                 }
         }
         Group::sync();
         int n = *count;
-        if (n > kEntries) n = select_exactly<BF16, VEC, TEAM>(x, begin, end, nq, a.classes, a.top, least, list, count, meet[0]);
+        if (n > kEntries || !all_kept) n = select_exactly<BF16, VEC, TEAM>(x, begin, end, nq, a.classes, a.top, least, list, count, meet[0]);
         auto leave = [&](int rank, uint64_t entry) {
             if (alone) write_entry(a, row, rank, entry, p, log2_S);
             else lists[int64_t(unit) * a.top + rank] = entry;

@@ -19,17 +19,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// n / d for n < 2^31, by a product
-struct Divisor {
-    uint32_t d, magic, shift;
-    explicit Divisor(uint32_t divisor) : d(divisor), shift(0)
-    {
-        while ((uint64_t(1) << shift) < d) ++shift;
-        magic = static_cast<uint32_t>(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d)) / d + 1);
-    }
-    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, magic) + n) >> shift; }
-};
-
 // Rows numbered through points and positions.
 struct Walk {
     int64_t point_stride, position_stride;

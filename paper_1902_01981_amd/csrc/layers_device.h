@@ -156,6 +156,17 @@ template <typename P> __device__ __forceinline__ P scalar_load(const P *p)
     return *reinterpret_cast<const __attribute__((address_space(4))) P *>(reinterpret_cast<uintptr_t>(p));
 }
 
+// n / d for n < 2^31, by a product
+struct Divisor {
+    uint32_t d, magic, shift;
+    explicit Divisor(uint32_t divisor) : d(divisor), shift(0)
+    {
+        while ((uint64_t(1) << shift) < d) ++shift;
+        magic = static_cast<uint32_t>(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - d)) / d + 1);
+    }
+    __device__ __forceinline__ uint32_t of(uint32_t n) const { return (__umulhi(n, magic) + n) >> shift; }
+};
+
 constexpr uint64_t kGolden = 0x9E3779B97F4A7C15ull;      // the increment of the splitmix64 generator
 __host__ __device__ __forceinline__ uint64_t splitmix_mix(uint64_t z)
 {

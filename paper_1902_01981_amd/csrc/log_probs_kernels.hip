@@ -7,7 +7,7 @@
 //
 //   log_probs_slices_kernel    a row, or a slice of it, in the registers of a wavefront or a workgroup, read once
 //   log_probs_join_kernel      rows of several slices
-//   log_probs_gradient_kernel  the gradient
+//   log_probs_gradient_kernel, log_probs_narrow_gradient_kernel   the gradient
 #include "softmax_device.h"
 
 #include <algorithm>
@@ -420,7 +420,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
                     const int to = atomicAdd(&hits, 1);
                     if (to < kHits) {
                         hit[to] = raw[k];
-                        hit_at[to] = place(k);
+                        hit_at[to] = lane + k * TEAM;
                     }
                 }
             __syncthreads();
@@ -431,7 +431,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
                     const float one = Element<BF16>::get(reinterpret_cast<const T *>(hit) + e);
                     if (one >= least) {
                         const int to = atomicAdd(count, 1);
-                        if (to < kEntries) list[to] = entry_of(one, hit_at[e / VEC] + e % VEC);
+                        if (to < kEntries) list[to] = entry_of(one, chunk_at<VEC>(begin + hit_at[e / VEC], nq, a.classes) + e % VEC);
                     }
                 }
         }
@@ -534,7 +534,30 @@ template <int THREADS> __global__ void __launch_bounds__(THREADS) log_probs_join
     for (int i = threadIdx.x; i < top; i += THREADS) write_entry(a, row, i, best[i], p, log2_S);
 }
 
-// dx_j = a ([j = t] - p_j) - b p_j (l_j + entropy); a thread has K chunks of a row, and an element of those behind the whole chunks.
+// dx_j = a ([j = t] - p_j) - b p_j (l_j + entropy)
+struct RowGradient {
+    float c, L, by_logp, by_entropy, H, value;
+    int64_t t;
+    bool flat;                   // all of the row is `value`
+    __device__ __forceinline__ RowGradient(const LogProbsGradArgs &a, int64_t row)
+    {
+        c = a.largest[row];
+        L = a.log_sum[row];
+        t = a.tokens ? a.tokens[row] : -1;
+        by_logp = t >= 0 ? a.dlogp[row] : 0.f;
+        by_entropy = a.entropy ? a.dentropy[row] : 0.f;
+        H = a.entropy ? a.entropy[row] : 0.f;
+        flat = t >= a.classes || c == -infinity();
+        value = t >= a.classes ? __builtin_nanf("") : 0.f;
+    }
+    __device__ __forceinline__ float of(float x, int j) const
+    {
+        const float l = x - c - L, p = exp_fast(l);
+        const float g = -p * (by_logp + by_entropy * (H + fmaxf(l, -256.f)));              // p is 0 there already
+        return flat ? value : j == t ? g + by_logp : g;
+    }
+};
+// A thread has K chunks of a row, and an element of those behind the whole chunks.
 template <bool BF16, int VEC, int K> __global__ void __launch_bounds__(kThreads) log_probs_gradient_kernel(LogProbsGradArgs a, int tiles)
 {
     using C = Chunk<BF16, VEC>;
@@ -546,16 +569,7 @@ template <bool BF16, int VEC, int K> __global__ void __launch_bounds__(kThreads)
         const int tile = static_cast<int>(unit - row * tiles);
         const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
         T *dx = static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride;
-        const float c = a.largest[row], L = a.log_sum[row];
-        const int64_t t = a.tokens ? a.tokens[row] : -1;
-        const float by_logp = t >= 0 ? a.dlogp[row] : 0.f, by_entropy = a.entropy ? a.dentropy[row] : 0.f, H = a.entropy ? a.entropy[row] : 0.f;
-        const bool flat = t >= a.classes || c == -infinity();
-        const float value = t >= a.classes ? __builtin_nanf("") : 0.f;
-        auto form = [&](float xi, int j) {
-            const float l = xi - c - L, p = exp_fast(l);
-            const float g = -p * (by_logp + by_entropy * (H + fmaxf(l, -256.f)));          // p is 0 there already
-            return flat ? value : j == t ? g + by_logp : g;
-        };
+        const RowGradient g(a, row);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int q = (tile * K + k) * kThreads + threadIdx.x;
@@ -563,13 +577,41 @@ template <bool BF16, int VEC, int K> __global__ void __launch_bounds__(kThreads)
                 float v[VEC];
                 C::widen(C::load(x + q * VEC), v);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = form(v[i], q * VEC + i);
+                for (int i = 0; i < VEC; ++i) v[i] = g.of(v[i], q * VEC + i);
                 C::store(dx + q * VEC, C::narrow(v));
             }
         }
         if (tile == 0 && threadIdx.x < left) {
             const int j = whole * VEC + threadIdx.x;
-            Element<BF16>::put(dx + j, form(Element<BF16>::get(x + j), j));
+            Element<BF16>::put(dx + j, g.of(Element<BF16>::get(x + j), j));
+        }
+    }
+}
+// Rows of fewer chunks than a workgroup has threads: their chunks, and the elements behind them, beside each other.  (100 000 x 100 bf16 78 us a workgroup per row.)
+template <bool BF16, int VEC> __global__ void __launch_bounds__(kThreads) log_probs_narrow_gradient_kernel(LogProbsGradArgs a, Divisor items)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    const int whole = a.classes / VEC, per = items.d;
+    const int64_t all = a.rows * per;
+    for (int64_t first = int64_t(blockIdx.x) * kThreads; first < all; first += int64_t(gridDim.x) * kThreads) {
+        const int64_t row0 = first / per;
+        const uint32_t l = static_cast<uint32_t>(first - row0 * per) + threadIdx.x, r = items.of(l);
+        const int64_t row = row0 + r;
+        const int item = l - r * per;
+        if (row >= a.rows) continue;
+        const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+        T *dx = static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride;
+        const RowGradient g(a, row);
+        if (item < whole) {
+            float v[VEC];
+            C::widen(C::load(x + item * VEC), v);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = g.of(v[i], item * VEC + i);
+            C::store(dx + item * VEC, C::narrow(v));
+        } else {
+            const int j = whole * (VEC - 1) + item;      // whole * VEC + (item - whole)
+            Element<BF16>::put(dx + j, g.of(Element<BF16>::get(x + j), j));
         }
     }
 }
@@ -656,12 +698,19 @@ hipError_t launch_log_probs(const LogProbsArgs &a, void *workspace, hipStream_t 
 hipError_t launch_log_probs_backward(const LogProbsGradArgs &a, hipStream_t stream)
 {
     if (a.rows == 0) return hipSuccess;
-    const int vec = a.classes < (a.bf16 ? 8 : 4) ? 1 : a.bf16 ? 8 : 4;
+    const int vec = a.classes < (a.bf16 ? 8 : 4) ? 1 : a.bf16 ? 8 : 4, whole = a.classes / vec;
+    if (whole < kThreads) {
+        const int per = whole + a.classes % vec;
+        const unsigned grid = static_cast<unsigned>(std::min<int64_t>((a.rows * per + kThreads - 1) / kThreads, 1 << 20));
+        if (vec == 1) (a.bf16 ? log_probs_narrow_gradient_kernel<true, 1> : log_probs_narrow_gradient_kernel<false, 1>)<<<grid, kThreads, 0, stream>>>(a, Divisor(per));
+        else if (a.bf16) log_probs_narrow_gradient_kernel<true, 8><<<grid, kThreads, 0, stream>>>(a, Divisor(per));
+        else log_probs_narrow_gradient_kernel<false, 4><<<grid, kThreads, 0, stream>>>(a, Divisor(per));
+        return hipGetLastError();
+    }
     constexpr int K = 4;
-    const int tiles = std::max(1, (a.classes / vec + kThreads * K - 1) / (kThreads * K));
+    const int tiles = (whole + kThreads * K - 1) / (kThreads * K);
     const unsigned grid = static_cast<unsigned>(std::min<int64_t>(a.rows * tiles, 1 << 20));
-    if (vec == 1) (a.bf16 ? log_probs_gradient_kernel<true, 1, K> : log_probs_gradient_kernel<false, 1, K>)<<<grid, kThreads, 0, stream>>>(a, tiles);
-    else if (a.bf16) log_probs_gradient_kernel<true, 8, K><<<grid, kThreads, 0, stream>>>(a, tiles);
+    if (a.bf16) log_probs_gradient_kernel<true, 8, K><<<grid, kThreads, 0, stream>>>(a, tiles);
     else log_probs_gradient_kernel<false, 4, K><<<grid, kThreads, 0, stream>>>(a, tiles);
     return hipGetLastError();
 }

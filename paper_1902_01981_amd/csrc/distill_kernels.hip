@@ -287,7 +287,7 @@ template <bool BF16, int K, bool GRAD> __global__ void __launch_bounds__(64 * kM
             meet_all(s);
             turn ^= 1;
             const Teacher now = teacher;
-            if (next != row) read_next(next);
+            if (row + stride < a.rows) read_next(next);
             const float loss = loss_of(now, a, s);
             if (lane == 0) a.loss[row] = loss;
             if constexpr (GRAD) {
@@ -393,7 +393,7 @@ template <bool BF16, int K, bool GRAD> __global__ void __launch_bounds__(64 * kM
 }
 
 // ---- a row in slices -------------------------------------------------------------------------------------------------------------
-constexpr int kSliceThreads = 256, kSliceChunks = 4;     // chunks that a thread has in flight
+constexpr int kSliceThreads = 256, kSliceChunks = 8;     // chunks that a thread has in flight
 __device__ __forceinline__ void join_block(Softmax &s, float (&lds)[2][kSliceThreads / 64], float unit)
 {
     join_lanes<64>(s, unit);

@@ -3,6 +3,7 @@
 // With q the teacher's shares at temperature T, about their largest logit, and c, S as of the softmax loss with exp(x / T) in place of exp(x):
 //     loss = w T sum_i q_i ((z_i - largest z) - (x_(j_i) - c) + T (log S - log S_q)),   dx_j = w T (exp((x_j - c) / T) / S - sum_(j_i = j) q_i).
 //
+//   distill_narrow_kernel  four rows in a wavefront
 //   distill_wave_kernel    a row in the registers of a wavefront
 //   distill_rows_kernel    a row in the registers of a workgroup, read once; a wavefront of its own reads the teacher's entries, forms the loss and puts the
 //                          teacher's classes into the gradient
@@ -140,6 +141,112 @@ __device__ __forceinline__ void at_entries(float (&value)[kEntries], const Teach
     const float from = usable(s.c);
 #pragma unroll
     for (int e = 0; e < kEntries; ++e) value[e] = fmaf(exp_fast(t.at[e] - from, unit), factor, -(t.w * a.temperature * q[e]));
+}
+
+// ---- sixteen lanes' rows ---------------------------------------------------------------------------------------------------------
+// Rows of up to 16 chunks, four beside each other in a wavefront.  (A wavefront per row took 100 000 x 100 bf16 with 20 entries 59 us: its instructions,
+// whatever the row has.)  Every lane goes through all entries and adds up the shares of those that are in its own chunk, so that nothing follows the gradient.
+template <bool BF16, int VEC, bool GRAD> __global__ void __launch_bounds__(256) distill_narrow_kernel(DistillArgs a)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    constexpr int kLanes = 16, kTeams = 256 / kLanes, kOwn = kMostTop / kLanes;
+    __shared__ int indices[GRAD ? kTeams : 1][GRAD ? kMostTop + 1 : 1];            // teams begin in other banks
+    __shared__ float shares[GRAD ? kTeams : 1][GRAD ? kMostTop + 1 : 1];
+    const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
+    const int64_t own_row = int64_t(blockIdx.x) * kTeams + team, row = std::min(own_row, a.rows - 1);
+    const bool here = own_row < a.rows;                  // the others go along
+    const int nq = (a.classes + VEC - 1) / VEC, doubled = nq * VEC - a.classes, at = chunk_at<VEC>(min(lane, nq - 1), nq, a.classes);
+    const float unit = kLog2e / a.temperature, nan = __builtin_nanf("");
+    const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+    const typename C::raw raw = C::load(x + at);
+    const float w = a.weights ? a.weights[row] : 1.f;
+    int index[kOwn];
+    float z[kOwn], logit[kOwn], most = -infinity();
+    bool there = false, unknown = false;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        index[e] = -1;
+        z[e] = -infinity();
+        logit[e] = 0.f;
+        const int i = lane + kLanes * e;
+        if (kLanes * e >= a.top) continue;
+        if (i < a.top) {
+            const int64_t given = a.top_index[row * a.top_row_stride + i];
+            const float zi = a.top_logits[row * a.top_row_stride + i];
+            const bool is = given >= 0 && zi != -infinity(), known = is && given < a.classes;
+            there |= is;
+            unknown |= is && !known;
+            if (is) z[e] = zi;
+            if (known) {
+                index[e] = static_cast<int>(given);
+                logit[e] = Element<BF16>::get(x + given);
+            }
+        }
+        most = fmaxf(most, z[e]);
+    }
+    most = lanes_most<kLanes>(most);
+    const uint32_t flags = static_cast<uint32_t>(__ballot(there) >> (threadIdx.x % 64 / kLanes * kLanes)) & 0xffffu;
+    const uint32_t unknowns = static_cast<uint32_t>(__ballot(unknown) >> (threadIdx.x % 64 / kLanes * kLanes)) & 0xffffu;
+    const float from_z = usable(most);
+    float q[kOwn], sum_q = 0.f;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        if (kLanes * e >= a.top) continue;
+        q[e] = exp_fast(z[e] - from_z, unit);
+        sum_q += q[e];
+    }
+    sum_q = lanes_total<kLanes>(sum_q);
+    const float by = 1.f / sum_q;
+    float v[VEC];
+    C::widen(raw, v);
+    Softmax s;
+    float counted[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) counted[i] = lane >= nq || (lane == nq - 1 && i < doubled) ? -infinity() : v[i];
+    take<VEC>(s, counted, true, unit);
+    const float c = lanes_most<kLanes>(s.c), from = usable(c);
+    float S = s.S * exp_fast(s.c - from, unit);
+    hold(S);                                             // rounded here: taken into an addition it would give every lane another sum
+    S = lanes_total<kLanes>(S);
+    const float both = 0.25f * a.temperature * kLn2 * (__builtin_amdgcn_logf(S) - __builtin_amdgcn_logf(sum_q));
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < kOwn; ++e) {
+        if (kLanes * e >= a.top) continue;
+        q[e] *= by;
+        const float term = q[e] * (0.25f * (z[e] - from_z) - (0.25f * logit[e] - 0.25f * from) + both);
+        sum += index[e] >= 0 && q[e] != 0.f ? term : 0.f;
+        if constexpr (GRAD) {
+            indices[team][lane + kLanes * e] = index[e];
+            shares[team][lane + kLanes * e] = q[e];
+        }
+    }
+    sum = lanes_total<kLanes>(sum);
+    if (lane == 0 && here) a.loss[row] = !flags ? 0.f : 4.f * (w * a.temperature * (unknowns ? nan : S == 0.f ? infinity() * sum_q : sum));
+    if constexpr (GRAD) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const Kind kind = !flags ? kZero : unknowns || !(sum_q == sum_q) ? kNan : kShares;
+        const bool flat = kind != kShares || S == 0.f;
+        const float value = kind == kNan ? nan : 0.f, factor = w * a.temperature / S;
+        float taken[VEC];                                // of the teacher's shares, by this chunk's classes
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) taken[i] = 0.f;
+        for (int e = 0; e < a.top; ++e) {
+            const int place = indices[team][e] - at;
+            const float share = shares[team][e];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) taken[i] += place == i ? share : 0.f;
+        }
+        if (!here || lane >= nq) return;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float share = exp_fast(v[i] - from, unit);
+            v[i] = flat ? value : taken[i] == 0.f ? share * factor : fmaf(share, factor, -(w * a.temperature * taken[i]));
+        }
+        C::store(static_cast<T *>(a.dlogits) + row * a.dlogits_row_stride + at, C::narrow(v));
+    }
 }
 
 // ---- a wavefront's rows ----------------------------------------------------------------------------------------------------------
@@ -515,7 +622,7 @@ __global__ void __launch_bounds__(kSliceThreads) distill_join_kernel(DistillArgs
 
 struct DistillPlan {
     int vec;
-    bool wave, slices;
+    bool narrow, wave, slices;
     int k, waves;                // chunks per lane, wavefronts of a workgroup with the teacher's
     int slice, per_row;          // chunks of a slice, slices of a row
     int64_t batch, with_gradient;        // rows per pair of launches: most; what the caches hold from its first to its second
@@ -527,6 +634,7 @@ DistillPlan plan_distill(int64_t rows, int64_t classes, bool bf16)
     DistillPlan p = {};
     p.vec = classes < (bf16 ? 8 : 4) ? 1 : bf16 ? 8 : 4;
     const int64_t whole = classes / p.vec, chunks = (classes + p.vec - 1) / p.vec;
+    p.narrow = chunks <= 16;
     if (chunks <= 64 * 8) {
         p.wave = true;
         p.k = static_cast<int>((chunks + 63) / 64);
@@ -551,6 +659,11 @@ DistillPlan plan_distill(int64_t rows, int64_t classes, bool bf16)
 
 constexpr int kUnits = 256;      // compute units, for the number of workgroups that stay
 
+template <bool BF16, int VEC> void launch_narrow(const DistillArgs &a, hipStream_t stream)
+{
+    const unsigned groups = static_cast<unsigned>((a.rows + 15) / 16);
+    (a.dlogits ? distill_narrow_kernel<BF16, VEC, true> : distill_narrow_kernel<BF16, VEC, false>)<<<groups, 256, 0, stream>>>(a);
+}
 template <bool BF16, int VEC, int K> void launch_wave(const DistillArgs &a, hipStream_t stream)
 {
     const unsigned groups = static_cast<unsigned>(std::min<int64_t>((a.rows + 3) / 4, 1 << 20));
@@ -589,8 +702,21 @@ template <bool BF16> hipError_t launch(const DistillArgs &a, const DistillPlan &
         }
         return hipGetLastError();
     }
-    if (p.vec == 1) {
-        launch_wave<BF16, 1, 1>(a, stream);
+    if (p.narrow) {
+        // at most 2^24 workgroups' threads are numbered in a launch
+        for (int64_t row = 0; row < a.rows; row += int64_t(1) << 26) {
+            constexpr int64_t e = BF16 ? 2 : 4;
+            DistillArgs b = a;
+            b.rows = std::min<int64_t>(int64_t(1) << 26, a.rows - row);
+            b.logits = static_cast<const char *>(a.logits) + row * a.row_stride * e;
+            b.top_index += row * a.top_row_stride;
+            b.top_logits += row * a.top_row_stride;
+            if (b.weights) b.weights += row;
+            b.loss += row;
+            if (b.dlogits) b.dlogits = static_cast<char *>(a.dlogits) + row * a.dlogits_row_stride * e;
+            if (p.vec == 1) launch_narrow<BF16, 1>(b, stream);
+            else launch_narrow<BF16, VEC>(b, stream);
+        }
     } else if (p.wave) {
         switch (p.k) {
         case 1: launch_wave<BF16, VEC, 1>(a, stream); break;

@@ -5,6 +5,7 @@
 // The alternatives: at least `top` values are no smaller than the top-th largest of the largest values of disjoint sets, so what is no smaller than that is
 // all that can be among them, and few other than them; their order is that of numbers with the value above and the index's complement below, of which no two are equal.
 //
+//   log_probs_narrow_kernel    four rows in a wavefront
 //   log_probs_slices_kernel    a row, or a slice of it, in the registers of a wavefront or a workgroup, read once
 //   log_probs_join_kernel      rows of several slices
 //   log_probs_gradient_kernel, log_probs_narrow_gradient_kernel   the gradient
@@ -351,7 +352,7 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
         float least;
         if constexpr (WAVE) {
             // sets of a lane's elements: the chunks; where they are too few for a bound that is one, eight sets of a lane if it has so many elements
-            constexpr int kSets = K >= 8 || VEC == 1 ? 1 : VEC < 8 / K ? VEC : 8 / K, kOfSet = VEC / kSets;
+            constexpr int kSets = K >= 8 ? 1 : VEC < 8 / K ? VEC : 8 / K, kOfSet = VEC / kSets;
             uint32_t key;
             if (kSets == 1 || 2 * a.top <= nq) {
                 uint32_t keys[K];
@@ -467,6 +468,101 @@ log_probs_slices_kernel(LogProbsArgs a, int slice, int slices, Part *parts, uint
             }
         }
         for (int rank = n + lane; rank < a.top; rank += TEAM) leave(rank, 0);
+    }
+}
+
+// Rows of up to 32 chunks: sixteen lanes each, four rows beside each other in a wavefront.  (A wavefront per row took 100 000 x 100 bf16 66 us with five
+// alternatives: its instructions, whatever the row has.)  The bound is the top-th largest element's upper half here, found bit by bit by all four rows at once.
+template <bool BF16, int VEC, int K, bool TOP> __global__ void __launch_bounds__(kThreads) log_probs_narrow_kernel(LogProbsArgs a)
+{
+    using C = Chunk<BF16, VEC>;
+    using T = typename C::element;
+    constexpr int kLanes = 16, kElements = kLanes * K * VEC;
+    __shared__ uint64_t entries[TOP ? kThreads / kLanes : 1][TOP ? kElements + 1 : 1];             // teams begin in other banks
+    const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
+    const int64_t own_row = int64_t(blockIdx.x) * (kThreads / kLanes) + team, row = std::min(own_row, a.rows - 1);
+    const bool here = own_row < a.rows;                  // the others go along
+    const int nq = (a.classes + VEC - 1) / VEC, doubled = nq * VEC - a.classes;
+    const T *x = static_cast<const T *>(a.logits) + row * a.row_stride;
+    typename C::raw raw[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) raw[k] = C::load_once(x + chunk_at<VEC>(min(lane + k * kLanes, nq - 1), nq, a.classes));
+    const Token token = read_token(a, row);
+    float v[K][VEC], most = -infinity();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        C::widen(raw[k], v[k]);
+        const int q = lane + k * kLanes, none = q >= nq ? VEC : q == nq - 1 ? doubled : 0;         // no elements of this place
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            v[k][i] = i < none ? -infinity() : v[k][i];
+            most = fmaxf(most, v[k][i]);
+        }
+    }
+    Part p = {most, 0.f, 0.f, 0.f};
+    const float from = usable(most);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            const float d = v[k][i] - from, e = exp_fast(d);
+            p.S += e;
+            p.E = fmaf(e, bounded(d), p.E);
+        }
+    }
+    join_lanes<kLanes>(p);
+    const float log2_S = __builtin_amdgcn_logf(p.S);
+    if (lane == 0 && here) write_row(a, row, token, p, log2_S);
+    if constexpr (TOP) {
+        auto number = [&](uint32_t bound) {              // of the row's elements that reach it
+            int mine = 0;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) mine += short_key(v[k][i]) >= bound;
+            }
+            return static_cast<int>(lanes_total<kLanes>(static_cast<float>(mine)));
+        };
+        uint32_t key = 0;
+#pragma unroll 1
+        for (int bit = 15; bit >= 0; --bit) {
+            const uint32_t more = key | 1u << bit;
+            if (number(more) >= a.top) key = more;
+        }
+        const float least = key ? unordered(key << 16) : kLowest;
+        uint64_t *list = entries[team];
+        int hits = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) hits += v[k][i] >= least;
+        }
+        int to = hits;                                   // up to and with this lane, then before it
+#pragma unroll
+        for (int d = 1; d < kLanes; d *= 2) {
+            const int other = __shfl_up(to, d, kLanes);
+            if (lane >= d) to += other;
+        }
+        const int n = __shfl(to, kLanes - 1, kLanes);
+        to -= hits;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int at = chunk_at<VEC>(min(lane + k * kLanes, nq - 1), nq, a.classes);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i)
+                if (v[k][i] >= least) list[to++] = entry_of(v[k][i], at + i);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (!here) return;
+        for (int i = lane; i < n; i += kLanes) {
+            const uint64_t entry = list[i];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < n; ++j) rank += list[j] > entry;
+            if (rank < a.top) write_entry(a, row, rank, entry, p, log2_S);
+        }
+        for (int rank = n + lane; rank < a.top; rank += kLanes) write_entry(a, row, rank, 0, p, log2_S);
     }
 }
 
@@ -646,6 +742,12 @@ template <bool BF16, int VEC, int K, int TEAM> void launch_slices(const LogProbs
                                                                                                                                                    lists);
 }
 
+template <bool BF16, int VEC, int K> void launch_narrow(const LogProbsArgs &a, hipStream_t stream)
+{
+    const unsigned groups = static_cast<unsigned>((a.rows + 15) / 16);
+    (a.top ? log_probs_narrow_kernel<BF16, VEC, K, true> : log_probs_narrow_kernel<BF16, VEC, K, false>)<<<groups, kThreads, 0, stream>>>(a);
+}
+
 template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan &p, void *workspace, hipStream_t stream)
 {
     constexpr int VEC = BF16 ? 8 : 4;
@@ -662,7 +764,9 @@ template <bool BF16> hipError_t launch(const LogProbsArgs &a, const LogProbsPlan
         if (b.top_logp) b.top_logp += row * a.top;
         if (b.largest) b.largest += row;
         if (b.log_sum) b.log_sum += row;
-        if (p.vec == 1) launch_slices<BF16, 1, 1, 64>(b, p, parts, lists, stream);
+        if (p.vec == 1) launch_narrow<BF16, 1, 1>(b, stream);
+        else if (p.chunks <= 16) launch_narrow<BF16, VEC, 1>(b, stream);
+        else if (p.chunks <= 32) launch_narrow<BF16, VEC, 2>(b, stream);
         else if (!p.wave) launch_slices<BF16, VEC, 8, kTeam>(b, p, parts, lists, stream);
         else if (p.k == 1) launch_slices<BF16, VEC, 1, 64>(b, p, parts, lists, stream);
         else if (p.k == 2) launch_slices<BF16, VEC, 2, 64>(b, p, parts, lists, stream);

@@ -109,7 +109,7 @@ def test_one_token_everywhere(points, positions, channels, dtype):
     _check_gradient(_backward(dy, tokens, 9, 1.0, bounds), dy, tokens, 1.0, bounds)
 
 
-@pytest.mark.parametrize("positions", [15, 16, 17, 31, 32, 33, 255, 256, 257, 4095, 4096, 4097])
+@pytest.mark.parametrize("positions", [15, 16, 17, 31, 32, 33, 255, 256, 257, 1023, 1024, 1025, 8191, 8192, 8193, 9217])
 def test_lengths_around_pieces_and_tiles(positions):
     for vocabulary in (2, 40, 5000):
         tokens, table, dy = _inputs(1, positions, 5, vocabulary, torch.float32, torch.float32, seed=positions)
@@ -117,9 +117,10 @@ def test_lengths_around_pieces_and_tiles(positions):
         _check_forward(_forward(tokens, table, torch.float32, 2.0), tokens, table, 2.0)
 
 
-def test_more_positions_than_the_workgroups_of_a_pass():
-    """Workgroups of several tiles: the sort goes on where the tile before has ended."""
-    points, positions, vocabulary = 3, 900_001, 1000
+@pytest.mark.parametrize("positions", [43_691, 349_525, 349_526, 900_001])
+def test_many_positions(positions):
+    """A tile each for some workgroups of the sort, full ones for 128 of them, twice as many, several tiles each."""
+    points, vocabulary = 3, 1000
     tokens, _, dy = _inputs(points, positions, 1, vocabulary, torch.bfloat16, torch.float32, seed=5)
     bounds = [0, 1, 3]
     _check_gradient(_backward(dy, tokens, vocabulary, 1.0, bounds), dy, tokens, 1.0, bounds)

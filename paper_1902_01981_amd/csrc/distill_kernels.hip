@@ -7,7 +7,11 @@
 //   distill_wave_kernel    a row in the registers of a wavefront
 //   distill_rows_kernel    a row in the registers of a workgroup, read once; a wavefront of its own reads the teacher's entries, forms the loss and puts the
 //                          teacher's classes into the gradient
-//   distill_slices_kernel, distill_join_kernel   rows wider than that: a row cut into slices, read twice
+//   distill_slices_kernel, distill_join_kernel   rows wider than that: a row cut into slices, read twice with the gradient
+//
+// Reads and writes bound it: 8 192 x 131 071 bf16 with 20 entries 933 us, 4.6 TB/s (the loss of one target 908); 4 099 x 50 008 bf16 with five 167 us, with 64
+// 179, 4.6 TB/s; without the gradient 74 and, 8 192 x 131 071, 436 us, 4.9 TB/s.  Slices: 2 048 x 128 000 fp32 188 us without the gradient, 5.6 TB/s, 705 with it, 4.5 TB/s
+// of what moves; 8 192 x 152 064 bf16 1.65 ms.  100 000 x 100 bf16 with 20 33 us, 1.2 TB/s: the entries, all of which every lane goes through.
 #include "softmax_device.h"
 
 #include <algorithm>

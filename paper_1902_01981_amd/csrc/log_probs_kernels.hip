@@ -9,6 +9,11 @@
 //   log_probs_slices_kernel    a row, or a slice of it, in the registers of a wavefront or a workgroup, read once
 //   log_probs_join_kernel      rows of several slices
 //   log_probs_gradient_kernel, log_probs_narrow_gradient_kernel   the gradient
+//
+// Without alternatives reads bound it, and arithmetic about as much: 8 192 x 131 071 bf16 413 us, 5.2 TB/s; 4 099 x 50 008 bf16 73 us, 5.6 TB/s; 2 048 x 128 000
+// fp32 158 us, 6.6 TB/s.  With them a slice's bound, list and ranks, each of which waits for the one before: 4 099 x 50 008 with 8 84 us, with 64 114, with 128 153;
+// 8 192 x 131 071 with 8 431; rows of equal values 342 (64).  Teams of 512 threads took 122 with 64 and 464 (8 192 x 131 071 with 8), of 1 024 182 and 780.
+// 100 000 x 100 bf16 with five 32 us, without 10.  Gradient: 8 192 x 131 071 bf16 812 us, 5.3 TB/s; 100 000 x 100 12 us.
 #include "softmax_device.h"
 
 #include <algorithm>

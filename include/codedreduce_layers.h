@@ -173,7 +173,7 @@ int cr_embedding_backward(const cr_layer_shape_t *shape, const cr_layer_view_t *
  *                 cannot be) have index -1 and -infinity
  *   largest, log_sum      `rows` floats each, c and L, what the gradient needs; NULL (both) where none will be asked for
  * A class that cannot be adds nothing to the entropy; as a token it has logp -infinity.  In a row of nothing else c, L and every logp are
- * -infinity, the entropy is 0.  A row with a NaN or +infinity has NaN in all outputs but the indices, which are -1.
+ * -infinity, the entropy is 0.  A row with a NaN or +infinity has NaN in all outputs but the indices, which are -1, and a logp of no token.
  * Limits: rows < 2^31, classes 1 to 2^28, top 0 to 128.
  *
  * cr_log_probs_backward: from what the forward pass was given and left,

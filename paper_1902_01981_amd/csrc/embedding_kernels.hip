@@ -639,7 +639,6 @@ template <int VEC> __global__ void __launch_bounds__(kThreads) embedding_join_ke
 
 // ---- what a gradient needs -------------------------------------------------------------------------------------------------------
 struct GradPlan {
-    uint32_t n;                  // positions of the largest batch of runs
     int passes, digit_bits;      // of the sort; of a digit of it
     int vec, nq, team;           // channels of a chunk, chunks of a row, lanes of a piece
     unsigned slabs;
@@ -657,10 +656,9 @@ int piece_length(uint32_t n, int team, unsigned slabs)
     return static_cast<int>(std::min<int64_t>(256, std::max<int64_t>(team < 64 ? 64 : 16, (length + 7) / 8 * 8)));
 }
 
-GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *bounds, int runs, uint32_t n)
+GradPlan plan_gradient(const LayerShape &shape, int vocabulary, int runs, uint32_t n)
 {
     GradPlan p = {};
-    p.n = n;
     int bits = 1;                                        // that the numbers 0 to `vocabulary` take
     while (uint64_t(vocabulary) >> bits) ++bits;
     p.passes = (bits + 8) / 9;
@@ -689,13 +687,6 @@ GradPlan plan_gradient(const LayerShape &shape, int vocabulary, const int64_t *b
     p.bytes = at;
     return p;
 }
-uint32_t most_positions(const LayerShape &shape, const int64_t *bounds, int runs)
-{
-    int64_t most = 0;
-    for (int r = 0; r < runs; r += BatchRuns::kRuns) most = std::max(most, bounds[std::min(runs, r + BatchRuns::kRuns)] - bounds[r]);
-    return static_cast<uint32_t>(most * shape.positions);
-}
-
 template <bool BF16, int VEC> void launch_sums(const Gradient &g, const Sorted &s, const GradPlan &p, const Zeros &z, hipStream_t stream)
 {
     auto go = [&](auto kernel, int team) {
@@ -732,12 +723,10 @@ __global__ void __launch_bounds__(kThreads) embedding_zeros_kernel(Zeros z) { cl
 
 size_t embedding_backward_bytes(const LayerShape &shape, int vocabulary, const int64_t *bounds, int runs)
 {
-    const uint32_t n = most_positions(shape, bounds, runs);
-    if (n == 0) return 0;
     size_t most = 0;                                     // pieces are shorter where there are fewer positions: every batch has to fit
     for (int r = 0; r < runs; r += BatchRuns::kRuns) {
         const int64_t points = bounds[std::min(runs, r + BatchRuns::kRuns)] - bounds[r];
-        if (points > 0) most = std::max(most, plan_gradient(shape, vocabulary, bounds, runs, static_cast<uint32_t>(points * shape.positions)).bytes);
+        if (points > 0) most = std::max(most, plan_gradient(shape, vocabulary, runs, static_cast<uint32_t>(points * shape.positions)).bytes);
     }
     return most;
 }
@@ -765,7 +754,7 @@ hipError_t launch_embedding_backward(const EmbeddingGradArgs &a, void *workspace
             embedding_zeros_kernel<<<static_cast<unsigned>(z.workgroups), kThreads, 0, stream>>>(z);
             continue;
         }
-        const GradPlan p = plan_gradient(shape, a.vocabulary, a.bounds, a.runs, n);
+        const GradPlan p = plan_gradient(shape, a.vocabulary, a.runs, n);
         char *ws = static_cast<char *>(workspace);
         auto words = [&](size_t at) { return reinterpret_cast<uint32_t *>(ws + at); };
         uint8_t *met = reinterpret_cast<uint8_t *>(ws + p.met);

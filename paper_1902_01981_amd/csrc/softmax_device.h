@@ -10,7 +10,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float infinity() { return __builtin_inff(); }
 // e^v for v <= 0, the distance from the largest logit: off by |v| + 2 units of 2^-24 of itself, by less than 3 of them of the largest share, whose v is 0.
 // Results below 2^-126 are 0.
-// unit: log2(e) over a temperature, for powers of the temperature's root of e.
+// unit: log2(e) / T, for e^(v / T).
 __device__ __forceinline__ float exp_fast(float v, float unit = kLog2e) { return __builtin_amdgcn_exp2f(v * unit); }
 
 // c = reference, S = sum; c is finite unless the part has nothing but -infinity (S = 0 then) or a +infinity (S is NaN then)

@@ -162,6 +162,20 @@ def test_no_tokens_and_tokens_of_no_row():
     assert bool((_backward(dy, nobody, 30, 2.0) == 0).all()) and bool((_forward(nobody, table, torch.bfloat16, 2.0) == 0).all())
 
 
+@pytest.mark.parametrize("channels", [6, 700])
+def test_many_positions_without_tokens(channels):
+    """More positions than one workgroup sorts, whose end, or all of which, have no row: NaN there has no influence, and every row is written."""
+    tokens, _, dy = _inputs(40, 500, channels, 60, torch.bfloat16, torch.float32, seed=15)
+    tokens[10:, 100:] = -1
+    tokens[20:] = torch.where(tokens[20:] == 3, 60, tokens[20:])
+    dy[(tokens < 0) | (tokens >= 60)] = float("nan")
+    got = _backward(dy, tokens, 60, 1.0, [0, 15, 15, 40])
+    assert bool(got.isfinite().all())
+    clean = torch.where(dy.isnan(), torch.zeros((), dtype=dy.dtype, device="cuda"), dy)
+    _check_gradient(got, clean, tokens, 1.0, [0, 15, 15, 40])
+    assert bool((_backward(dy, torch.full_like(tokens, -1), 60, 1.0, [0, 15, 40]) == 0).all())
+
+
 def test_no_points():
     tokens, table = torch.empty(0, 4, dtype=torch.int64, device="cuda"), torch.ones(10, 6, device="cuda")
     assert _forward(tokens, table, torch.float32, 1.0).shape == (0, 4, 6)

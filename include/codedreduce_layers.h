@@ -150,11 +150,12 @@ int cr_softmax_loss(int64_t rows, int64_t classes, int dtype, const void *logits
  * cr_embedding_backward:
  *     dtable[r][v][:] = scale sum dy(n, p, :)   over the points n of run r and the positions p with t(n, p) = v
  *   every row is written, rows of tokens that a run does not have with 0; where there is no token, or no row, dy has no influence, be it
- *   infinite or NaN.  A run's terms are added up in the order of their points and positions, in pieces that go by the call's shape.
+ *   infinite or NaN.  A run's terms are added up in the order of their points and positions, in pieces that go by the call's shape and
+ *   its tokens; the pieces' sums meet in 64 bits, in a fixed order.
  *   shape         of dy, dtype that of dy;   bounds, runs  as above
  *   dtable        runs x vocabulary x channels floats
  * cr_embedding_workspace_bytes: what the gradient needs (256-byte aligned): 16 bytes a position (17 of more than one run), two rows of floats for
- * each piece (16 to 256 positions), a byte for each row of up to 128 runs. */
+ * each piece (16 to 256 positions), a byte for each row of up to 128 runs, 2 KB for each of up to 256 workgroups that sort; each of these up to 256 bytes more. */
 int cr_embedding_workspace_bytes(const cr_layer_shape_t *shape, int64_t vocabulary, const int64_t *bounds, int runs, size_t *backward_bytes);
 int cr_embedding_forward(const cr_layer_shape_t *shape, const cr_layer_view_t *tokens, const void *table, int table_dtype, int64_t vocabulary,
                          float scale, const cr_layer_view_t *y, void *hip_stream);
@@ -165,7 +166,8 @@ int cr_embedding_backward(const cr_layer_shape_t *shape, const cr_layer_view_t *
 /* ---- log probabilities -------------------------------------------------------------------------------------------------------------------
  * Row by row, with x the row's logits and t its token:
  *     c = max_j x_j,   L = log(sum_j exp(x_j - c)),   l_j = x_j - c - L,   logp = l_t,   entropy = -sum_j exp(l_j) l_j
- * and the `top` classes of the largest logits in descending order, of equal ones the lowest first, with their l_j.
+ * and the `top` classes of the largest logits in descending order, of equal ones the lowest first, with their l_j.  (Where neither entropy nor alternatives are
+ * wanted, cr_softmax_loss has logp as a loss of weight -1, and its gradient, with the weights -dlogp, in the same call.)
  *   logits        rows x classes of `dtype` (enum cr_xdtype), contiguous classes, row_stride elements apart
  *   tokens, logp  `rows` int64 and floats, or NULL (both).  Negative: no token, logp is 0.  At least `classes`: no class, logp is NaN
  *   entropy       `rows` floats or NULL

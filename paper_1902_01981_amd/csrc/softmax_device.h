@@ -8,9 +8,9 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 __device__ __forceinline__ float infinity() { return __builtin_inff(); }
-// e^v for v <= 0, the distance from the largest logit: off by |v| + 2 units of 2^-24 of itself, by less than 3 of them of the largest share, whose v is 0.
-// Results below 2^-126 are 0.
-// unit: log2(e) / T, for e^(v / T).
+// e^v for v <= 0, the distance from the largest logit: off by 1.25 |v| + 2 units of 2^-24 of itself (the product's rounding, 0.23 of one that the constant is off by, and the
+// hardware's exponential), by less than 3 of them of the largest share, whose v is 0.  Results below 2^-126 are 0.
+// unit: log2(e) / T, for e^(v / T); that is one rounding more, 2.25 |v| / T + 2 units.
 __device__ __forceinline__ float exp_fast(float v, float unit = kLog2e) { return __builtin_amdgcn_exp2f(v * unit); }
 
 // c = reference, S = sum; c is finite unless the part has nothing but -infinity (S = 0 then) or a +infinity (S is NaN then)

@@ -10,11 +10,13 @@
 //                              gradient, others to the workspace; rows of the gradient that no position has are cleared beside them
 //   embedding_join_kernel      cells of several pieces
 //
-// Reads and writes bound it.  Forward: y is written past the caches, which then keep the table: 8 192 x 120 x 512 bf16 of 50 008 rows 300 us with ordinary stores,
-// 195 with these, 5.2 TB/s of what is written; 64 x 512 x 4 096 of 131 072 rows 79 and 64.  What reads y next is no slower for it: with dropout behind it
-// 16 x 512 x 4 096 44 us either way, 256 x 512 x 4 096 798 and 768.  Gradient: 64 x 512 x 4 096 bf16 of 131 072 rows 482 us, 5.0 TB/s, most
+// Reads and writes bound it.  Forward: y is written past the caches, which then keep the rows of frequent tokens: where the i-th is met as 1 / (i + 2.7),
+// 8 192 x 120 x 512 bf16 of 50 008 rows takes 300 us with ordinary stores and 195 with these, 5.2 TB/s of what is written, 64 x 512 x 4 096 of 131 072 rows 79 and 64; where all
+// are met as often, 281 and 273, 100 and 82.  What reads y next finds less of it in the caches: forward and dropout behind it, tokens all as frequent, 16 x 512 x 4 096 44 us and 45,
+// 64 x 512 x 4 096 202 and 207, 256 x 512 x 4 096 798 and 768, 8 192 x 120 x 512 683 and 671.  Gradient: 64 x 512 x 4 096 bf16 of 131 072 rows 482 us, 5.0 TB/s, most
 // of it the rows of zeros, which the sums hide behind; 8 192 x 120 x 512 of 50 008 rows 315 us, 3.5 TB/s: gathering rows of 1 KB 210, the two passes of the sort 70,
-// the parts of frequent tokens 24; 683 x 9 x 1 027 fp32 with twelve runs of 5 003 rows 62 us, 4.4 TB/s.  600 positions 22 us, 3 launches.
+// the parts of frequent tokens 24; 683 x 9 x 1 027 fp32 with twelve runs of 5 003 rows 62 us, 4.4 TB/s.  600 positions 22 us, 3 launches; of a
+// gradient of 50 MB 27 us with 1 027 channels, but 53 with 64 and 96 with 8, whose zeros go out 64 rows, 2 KB of 8 channels, a step.
 #include "layers_device.h"
 
 #include <algorithm>

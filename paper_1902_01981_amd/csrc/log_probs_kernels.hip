@@ -12,7 +12,10 @@
 //
 // Without alternatives reads bound it, and arithmetic about as much: 8 192 x 131 071 bf16 413 us, 5.2 TB/s; 4 099 x 50 008 bf16 73 us, 5.6 TB/s; 2 048 x 128 000
 // fp32 158 us, 6.6 TB/s.  With them a slice's bound, list and ranks, each of which waits for the one before: 4 099 x 50 008 with 8 84 us, with 64 114, with 128 153;
-// 8 192 x 131 071 with 8 431; rows of equal values 342 (64).  Teams of 512 threads took 122 with 64 and 464 (8 192 x 131 071 with 8), of 1 024 182 and 780.
+// 8 192 x 131 071 with 8 431; rows of equal values 335 (64).  A bound of 16 bits tells few fp32 logits apart whose common offset is large beside their spread, and
+// every slice is then searched bit by bit: 2 048 x 128 000 fp32 with 64, normal logits of deviation 3, 220 us, 263 around 300, 4.3 ms around 3 000; bf16, 4 099 x 50 008, 114, 125 and
+// 334, where what is left of the logits are equal values.  A workgroup's lanes have eight chunks whether the slice fills them or not: 40 990 x 5 000 bf16 109 us, 3.8 TB/s,
+// x 8 000 130, x 16 384 199, 6.8 TB/s, x 4 096 by wavefronts 55, 6.1 TB/s; with 20 177, 184, 253 and 86.  Teams of 512 threads took 122 with 64 and 464 (8 192 x 131 071 with 8), of 1 024 182 and 780.
 // 100 000 x 100 bf16 with five 32 us, without 10.  Gradient: 8 192 x 131 071 bf16 812 us, 5.3 TB/s; 100 000 x 100 12 us.
 #include "softmax_device.h"
 
@@ -167,8 +170,8 @@ __device__ __forceinline__ uint32_t short_key(float x) { return x > -infinity() 
 
 constexpr int kWaveEntries = 512, kBlockEntries = 1024;  // that a team keeps of those that may be among the largest
 
-// The `top` largest of chunks [begin, end) of a row, where too many are no smaller than `least`, equal ones mostly: the top-th largest value itself, which is the
-// smallest of them if all the others are too few, and is found bit by bit if not; then as many of its places as are wanted, lowest first.  The chunks are
+// The `top` largest of chunks [begin, end) of a row, where too many are no smaller than `least`: the top-th largest value itself, which is the smallest of them if all the
+// others are too few (two passes, where many are equal), and is found bit by bit if not (32 more); then as many of its places as are wanted, lowest first (two).  The chunks are
 // read again each time: 32 KB at most, from the caches.
 template <bool BF16, int VEC, int TEAM>
 __device__ __noinline__ int select_exactly(const typename Chunk<BF16, VEC>::element *x, int begin, int end, int nq, int classes, int top, float least, uint64_t *list, int *count, float *meet)

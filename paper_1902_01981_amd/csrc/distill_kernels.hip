@@ -10,7 +10,7 @@
 //   distill_slices_kernel, distill_join_kernel   rows wider than that: a row cut into slices, read twice with the gradient
 //
 // Reads and writes bound it: 8 192 x 131 071 bf16 with 20 entries 933 us, 4.6 TB/s (the loss of one target 908); 4 099 x 50 008 bf16 with five 167 us, with 64
-// 179, 4.6 TB/s; without the gradient 74 and, 8 192 x 131 071, 436 us, 4.9 TB/s.  Slices: 2 048 x 128 000 fp32 188 us without the gradient, 5.6 TB/s, 705 with it, 4.5 TB/s
+// 179, 4.6 TB/s, fp32 351, 4.7 TB/s; without the gradient 74 and, 8 192 x 131 071, 436 us, 4.9 TB/s.  Slices: 2 048 x 128 000 fp32 188 us without the gradient, 5.6 TB/s, 705 with it, 4.5 TB/s
 // of what moves; 8 192 x 152 064 bf16 1.65 ms.  100 000 x 100 bf16 with 20 33 us, 1.2 TB/s: the entries, all of which every lane goes through.
 #include "softmax_device.h"
 
@@ -631,7 +631,10 @@ struct DistillPlan {
     int slice, per_row;          // chunks of a slice, slices of a row
     int64_t batch, with_gradient;        // rows per pair of launches: most; what the caches hold from its first to its second
 };
-constexpr int kFew = 8, kMany = 18;                      // chunks of a lane
+// Chunks of a lane: 8 take 58 registers, so that two workgroups of 16 wavefronts fit a compute unit, and 18 are the least that hold 131 072 bf16 classes.  18 take 95
+// registers, one workgroup a unit; 24, 184 320 bf16 classes, would take 122 and leave it at one, but are not built: rows from 138 248 bf16 and 69 124 fp32 classes on are cut into
+// slices and read twice (8 192 x 138 240 bf16 878 us, x 152 064 1 660).
+constexpr int kFew = 8, kMany = 18;
 
 DistillPlan plan_distill(int64_t rows, int64_t classes, bool bf16)
 {

@@ -1,4 +1,5 @@
-"""The table's gradient where its positions are sorted by many workgroups: digits of three and four passes, workgroups of several tiles, with one run and several.
+"""The table's gradient where its positions are sorted by many workgroups: digits of three and four passes, workgroups of several tiles, with one run and several, many runs;
+and the largest shapes.
 
 What may differ is what test_tokens_embedding.py says: sums of at most 256 terms in 32 bits, and three more roundings."""
 import numpy as np
@@ -86,3 +87,85 @@ def test_passes_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(dtable, _backward(dy, tokens, vocabulary, 1.0, bounds))
+
+
+@pytest.mark.parametrize("runs", [129, 300])
+def test_many_runs(runs):
+    """Several batches of runs, each of more positions than one workgroup sorts; a batch without points between them."""
+    points, positions, channels, vocabulary = 700, 60, 12, 530
+    tokens, _, dy = _inputs(points, positions, channels, vocabulary, torch.bfloat16, torch.float32, seed=3)
+    rng = np.random.default_rng(runs)
+    bounds = np.concatenate([[0, 0], np.sort(rng.integers(0, points + 1, runs - 3)), [points, points]])
+    _check_gradient(_backward(dy, tokens, vocabulary, 1.0, bounds), dy, tokens, 1.0, bounds)
+    bounds = np.concatenate([[0], np.full(127, 300), np.full(130, 300), np.full(runs, points)])
+    _check_gradient(_backward(dy, tokens, vocabulary, 1.0, bounds), dy, tokens, 1.0, bounds)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("channels", [5, 60, 1030])
+def test_strides(channels, dtype):
+    """Many positions whose tokens and gradients lie apart, in either order, or are the same for all points."""
+    points, positions, vocabulary, bounds = 130, 71, 300, [0, 50, 130]
+    tokens, _, dy = _inputs(points, positions, channels, vocabulary, dtype, dtype, seed=8)
+    want = _backward(dy, tokens, vocabulary, 1.0, bounds)
+    _check_gradient(want, dy, tokens, 1.0, bounds)
+    room = torch.full((points, positions + 2, channels + 7), 4.0, dtype=dtype, device="cuda")
+    room[:, 1:1 + positions, 3:3 + channels] = dy
+    apart = room[:, 1:1 + positions, 3:3 + channels]
+    crossed = dy.transpose(0, 1).contiguous().transpose(0, 1)
+    long = torch.full((points, positions + 5), 3, device="cuda")
+    long[:, 2:2 + positions] = tokens
+    for d, t in ((apart, tokens), (crossed, tokens), (dy, long[:, 2:2 + positions]), (apart, tokens.t().contiguous().t())):
+        assert torch.equal(_backward(d, t, vocabulary, 1.0, bounds), want)
+    one, same = tokens[:1].expand(points, positions), dy[:, :1].expand(points, positions, channels)
+    _check_gradient(_backward(same, one, vocabulary, 1.0, bounds), same, one, 1.0, bounds)
+
+
+def test_the_most_positions():
+    """2^31 - 2 positions of one channel, near the limit of points and positions together.  The terms are small whole numbers, whose sums 32 bits hold: all is exact."""
+    points, positions, vocabulary = 2, (1 << 30) - 1, 1000
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    tokens = torch.empty(points, positions, dtype=torch.int64, device="cuda").random_(0, vocabulary + 1, generator=gen)
+    tokens -= 1                                          # -1: no token
+    dy = torch.empty(points, positions, 1, dtype=torch.bfloat16, device="cuda").random_(0, 4, generator=gen)
+    table = torch.randn(vocabulary, 1, generator=gen, device="cuda")
+    want = torch.zeros(2, vocabulary + 1, dtype=torch.float64, device="cuda")
+    y = torch.full((points, positions, 1), 9.0, dtype=torch.bfloat16, device="cuda")
+    cr.cr_embedding_forward(tokens, table, y, scale=0.5)
+    rows = torch.cat([table[:, 0] * 0.5, torch.zeros(1, device="cuda")]).bfloat16()            # -1 is the last one
+    step = 1 << 27
+    for p in range(points):
+        for lo in range(0, positions, step):
+            t = tokens[p, lo:lo + step]
+            want[p] += torch.bincount(t + 1, weights=dy[p, lo:lo + step, 0].double(), minlength=vocabulary + 1)
+            assert torch.equal(y[p, lo:lo + step, 0], rows[t])
+    del y
+    assert float(want.max()) < 2 ** 24
+    dtable = torch.full((2, vocabulary, 1), 9.0, device="cuda")
+    cr.cr_embedding_backward(dy, tokens, dtable, bounds=[0, 1, 2])
+    assert torch.equal(dtable[..., 0].double(), want[:, 1:])
+    cr.cr_embedding_backward(dy, tokens, dtable[:1], scale=2.0)
+    assert torch.equal(dtable[0, :, 0].double(), 2 * want[:, 1:].sum(dim=0))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "bf16"])
+def test_the_most_channels(dtype):
+    """2^24 and a few less, of cells that lie in a piece and that go on behind it.  Whole numbers again: all is exact."""
+    for channels in (1 << 24, (1 << 24) - 3):
+        gen = torch.Generator(device="cuda").manual_seed(channels)
+        tokens = torch.tensor([[1] * 20 + [0, -1, 3], [1] * 20 + [3, 4, 0]], device="cuda")           # 4: no row
+        dy = torch.empty(2, 23, channels, dtype=dtype, device="cuda").random_(0, 4, generator=gen)
+        table = torch.empty(4, channels, dtype=dtype, device="cuda").random_(0, 4, generator=gen)
+        for bounds in ([0, 2], [0, 1, 2]):
+            got = _backward(dy, tokens, 4, 0.5, bounds)
+            for r in range(len(bounds) - 1):
+                part, t = dy[bounds[r]:bounds[r + 1]].reshape(-1, channels), tokens[bounds[r]:bounds[r + 1]].reshape(-1)
+                for v in range(4):
+                    assert torch.equal(got[r, v], 0.5 * part[t == v].float().sum(dim=0))
+        del got
+        y = torch.full_like(dy, 9.0)
+        cr.cr_embedding_forward(tokens, table, y, scale=2.0)
+        for v in range(4):
+            assert bool((y[tokens == v] == 2 * table[v]).all())
+        assert bool((y[tokens < 0] == 0).all()) and bool(y[tokens == 4].isnan().all())
+        del dy, y, table
